@@ -55,6 +55,8 @@ extern "C" {
 #define VZ_OP_DECODE 1
 #define VZ_OP_EVICT 2
 #define VZ_OP_DECODE_EVICT 3   /* voxzip_decode_evict */
+#define VZ_OP_DECODE_Q4 4        /* voxzip_decode_attend_score_q4 (and its ragged twin) */
+#define VZ_OP_DECODE_EVICT_Q4 5  /* voxzip_decode_evict_q4 */
 
 /*
  * Stage-1 span offsets (Sec. 3.2.1: confidence filter, Eq. 3 time-to-token
@@ -378,6 +380,132 @@ VZ_API int voxzip_evict_compact_ragged(void *k_cache, void *v_cache, float *scor
                                        int32_t *new_len_out, int32_t *status, int32_t n_layers,
                                        int32_t kv_heads, int32_t d, int32_t dtype, void *workspace,
                                        size_t ws_bytes, void *stream);
+
+/*
+ * 4-bit caches
+ * ------------
+ * The *_q4 entry points keep the cache in 4 bits: 0.53 bytes per element
+ * against 2 (bfloat16), so a decode step reads, and a GPU holds, 3.76 times
+ * less of it.  They are the operations of the entry points above on another
+ * cache; q, k_new, v_new, inputs of fusion and outputs stay `dtype`.
+ *
+ *  Format: a row of d channels is d / 2 bytes of codes and d / 32 scale bytes,
+ *  in planes of their own: codes uint8 [n_layers][kv_heads][cap][d / 2],
+ *  scales uint8 [n_layers][kv_heads][cap][d / 32] (ragged: total for cap).
+ *  Channel 2 i is the low half of code byte i, channel 2 i + 1 the high half;
+ *  code c stands for 0, 1/2, 1, 3/2, 2, 3, 4, 6 (c = 0 .. 7) and their
+ *  negatives (c = 8 .. 15), times 2^(b - 127), b the scale byte of the
+ *  channel's block of 32.  b = 255: the block reads as NaN.  Bytes 2 .. 252
+ *  and 255 are written; zero-filled memory reads as zeros.  (E2M1 elements
+ *  with an E8M0 scale.)
+ *  Quantising a row: per block e is the smallest of -125 .. 125 with
+ *  max |x| <= 7 * 2^e (125 if there is none), b = e + 127, and each channel
+ *  gets the code nearest x / 2^e, ties to the even code, at most 6 in
+ *  magnitude.  A block with an infinity or a NaN gets b = 255.
+ *  Every value is exact in bfloat16 and float32.
+ *  Codes must lie on 16-byte boundaries, scales on d / 32-byte ones
+ *  (VZ_ERR_INVALID).
+ */
+
+/*
+ * Stage-1 fusion into a 4-bit cache: each span's mean (plus its anchor) is
+ * quantised as it is formed, with no rounding to dtype between: the codes are
+ * those of (sum of the span's rows + n anchor) / n, n the span's length, with
+ * 64-bit sums.  Spans of length 1 pack rows as they are.
+ *  k_in, v_in   as for voxzip_fuse_spans (both given; d in {64, 128}).
+ *  score_out, pos_out, the offsets and the errors: as there.
+ */
+VZ_API int voxzip_fuse_spans_q4(const void *k_in, const void *v_in, int32_t T_in,
+                                const int32_t *span_off, int32_t n_spans, const void *anchor_k,
+                                const void *anchor_v, void *k_codes, void *k_scales, void *v_codes,
+                                void *v_scales, float *score_out, int32_t *pos_out,
+                                int32_t n_layers, int32_t kv_heads, int32_t d, int32_t cap_out,
+                                int32_t dtype, void *stream);
+
+/*
+ * The values of n_rows rows of a 4-bit cache: out [n_rows][d] in dtype, exact.
+ *  codes [n_rows][d / 2], scales [n_rows][d / 32]: e.g. whole K planes, with
+ *  n_rows = n_layers kv_heads cap.  codes must lie on 4-byte boundaries, out
+ *  on 16-byte ones; n_rows <= 2^28.
+ * Errors: VZ_ERR_INVALID (null pointer, alignment, aliasing), VZ_ERR_SHAPE,
+ * VZ_ERR_UNSUPPORTED.
+ */
+VZ_API int voxzip_unpack_q4(const void *codes, const void *scales, int64_t n_rows, int32_t d,
+                            void *out, int32_t dtype, void *stream);
+
+/*
+ * One decode step over a 4-bit cache: voxzip_decode_attend_score, where the
+ * new K and V rows are quantised into slot len and attention reads what the
+ * cache holds, the new slot included.  dtype is the type of q, k_new, v_new
+ * and out.  Logits, softmax statistics, probabilities in the score and sums
+ * are float32 in both types; the probabilities of P V have 8 bits (bfloat16)
+ * or 24 (float32).
+ *  workspace    at least voxzip_workspace_bytes(VZ_OP_DECODE_Q4, ...) bytes.
+ * Errors: as voxzip_decode_attend_score.
+ */
+VZ_API int voxzip_decode_attend_score_q4(const void *q, const void *k_new, const void *v_new,
+                                         void *k_codes, void *k_scales, void *v_codes,
+                                         void *v_scales, float *score, int32_t *pos, void *out,
+                                         int32_t len, int32_t next_pos, float gamma, float sm_scale,
+                                         int32_t n_layers, int32_t n_q_heads, int32_t kv_heads,
+                                         int32_t d, int32_t cap, int32_t dtype, void *workspace,
+                                         size_t ws_bytes, void *stream);
+
+/*
+ * Stage-2 eviction of a 4-bit cache: voxzip_evict_compact, the moved rows
+ * being codes and scales.  workspace: VZ_OP_EVICT.  Errors: as there.
+ */
+VZ_API int voxzip_evict_compact_q4(void *k_codes, void *k_scales, void *v_codes, void *v_scales,
+                                   float *score, int32_t *pos, int32_t len, int32_t budget,
+                                   int32_t n_sink, int32_t n_recent, int32_t next_pos,
+                                   int32_t *kept_pos_out, int32_t *new_len_out, int32_t n_layers,
+                                   int32_t kv_heads, int32_t d, int32_t cap, void *workspace,
+                                   size_t ws_bytes, void *stream);
+
+/*
+ * One generation step over a 4-bit cache: voxzip_decode_attend_score_q4, then
+ * voxzip_evict_compact_q4 of the len + 1 slots it leaves, with the results of
+ * the two calls, bit for bit (as voxzip_decode_evict).
+ *  workspace    at least voxzip_workspace_bytes(VZ_OP_DECODE_EVICT_Q4, ...) bytes.
+ */
+VZ_API int voxzip_decode_evict_q4(const void *q, const void *k_new, const void *v_new,
+                                  void *k_codes, void *k_scales, void *v_codes, void *v_scales,
+                                  float *score, int32_t *pos, void *out, int32_t len,
+                                  int32_t next_pos, float gamma, float sm_scale, int32_t budget,
+                                  int32_t n_sink, int32_t n_recent, int32_t *kept_pos_out,
+                                  int32_t *new_len_out, int32_t n_layers, int32_t n_q_heads,
+                                  int32_t kv_heads, int32_t d, int32_t cap, int32_t dtype,
+                                  void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Ragged twins over a packed 4-bit cache (codes [n_layers][kv_heads][total][d / 2],
+ * scales [n_layers][kv_heads][total][d / 32]); per-sequence arrays, status and
+ * errors as for the ragged twins above.  Anchors of the fusion are laid out
+ * [n_layers][kv_heads][total][d].  Workspaces: VZ_OP_DECODE_Q4 and VZ_OP_EVICT.
+ * A sequence's outputs agree with a single-sequence call's to float32 rounding
+ * (chunks of other sizes are added up), its appended rows bit for bit.
+ */
+VZ_API int voxzip_fuse_spans_q4_ragged(
+    const void *k_in, const void *v_in, const int64_t *in_base, const int32_t *T_in,
+    int64_t total_in, const int32_t *span_off, const int64_t *off_base, const int32_t *n_spans,
+    int64_t total_off, int32_t max_spans, const void *anchor_k, const void *anchor_v,
+    void *k_codes, void *k_scales, void *v_codes, void *v_scales, float *score_out,
+    int32_t *pos_out, const int64_t *seq_base, const int32_t *cap, int64_t total, int32_t n_seqs,
+    int32_t *status, int32_t n_layers, int32_t kv_heads, int32_t d, int32_t dtype, void *stream);
+
+VZ_API int voxzip_decode_attend_score_q4_ragged(
+    const void *q, const void *k_new, const void *v_new, void *k_codes, void *k_scales,
+    void *v_codes, void *v_scales, float *score, int32_t *pos, void *out, const int64_t *seq_base,
+    const int32_t *cap, const int32_t *len, const int32_t *next_pos, int64_t total, int32_t n_seqs,
+    float gamma, float sm_scale, int32_t n_layers, int32_t n_q_heads, int32_t kv_heads, int32_t d,
+    int32_t dtype, int32_t *status, void *workspace, size_t ws_bytes, void *stream);
+
+VZ_API int voxzip_evict_compact_q4_ragged(
+    void *k_codes, void *k_scales, void *v_codes, void *v_scales, float *score, int32_t *pos,
+    const int64_t *seq_base, const int32_t *cap, const int32_t *len, const int32_t *budget,
+    const int32_t *next_pos, int64_t total, int32_t n_seqs, int32_t n_sink, int32_t n_recent,
+    int32_t *kept_pos_out, int32_t *new_len_out, int32_t *status, int32_t n_layers,
+    int32_t kv_heads, int32_t d, void *workspace, size_t ws_bytes, void *stream);
 
 /* Text of a status code (static storage). */
 VZ_API const char *voxzip_status_string(int status);

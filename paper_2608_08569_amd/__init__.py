@@ -19,6 +19,7 @@ VZ_ERR_UNSUPPORTED, VZ_ERR_HIP, VZ_ERR_WORKSPACE = -4, -5, -6
 VZ_IDLE = 1  # per-sequence status of a ragged call: an idle batch slot (cap 0)
 VZ_F32, VZ_BF16 = 0, 1
 VZ_OP_DECODE, VZ_OP_EVICT, VZ_OP_DECODE_EVICT = 1, 2, 3
+VZ_OP_DECODE_Q4, VZ_OP_DECODE_EVICT_Q4 = 4, 5
 VZ_NOALLOC_SCRATCH_BYTES = 64 << 20
 
 _lib = None
@@ -62,8 +63,25 @@ def lib() -> ctypes.CDLL:
                                                     i32, i32, i32, i32, i32, P, P, sz, P]
     L.voxzip_evict_compact_ragged.argtypes = [P, P, P, P, P, P, P, P, P, i64, i32, i32, i32, P, P, P,
                                               i32, i32, i32, i32, P, sz, P]
+    L.voxzip_fuse_spans_q4.argtypes = [P, P, i32, P, i32, P, P, P, P, P, P, P, P, i32, i32, i32, i32, i32, P]
+    L.voxzip_unpack_q4.argtypes = [P, P, i64, i32, P, i32, P]
+    L.voxzip_decode_attend_score_q4.argtypes = [P, P, P, P, P, P, P, P, P, P, i32, i32, f32, f32,
+                                                i32, i32, i32, i32, i32, i32, P, sz, P]
+    L.voxzip_evict_compact_q4.argtypes = [P, P, P, P, P, P, i32, i32, i32, i32, i32, P, P, i32, i32, i32, i32, P, sz,
+                                          P]
+    L.voxzip_decode_evict_q4.argtypes = [P, P, P, P, P, P, P, P, P, P, i32, i32, f32, f32, i32, i32, i32, P, P,
+                                         i32, i32, i32, i32, i32, i32, P, sz, P]
+    L.voxzip_fuse_spans_q4_ragged.argtypes = [P, P, P, P, i64, P, P, P, i64, i32, P, P, P, P, P, P, P, P, P, P, i64,
+                                              i32, P, i32, i32, i32, i32, P]
+    L.voxzip_decode_attend_score_q4_ragged.argtypes = [P, P, P, P, P, P, P, P, P, P, P, P, P, P, i64, i32, f32, f32,
+                                                       i32, i32, i32, i32, i32, P, P, sz, P]
+    L.voxzip_evict_compact_q4_ragged.argtypes = [P, P, P, P, P, P, P, P, P, P, P, i64, i32, i32, i32, P, P, P,
+                                                 i32, i32, i32, P, sz, P]
     for f in (L.voxzip_fuse_spans, L.voxzip_decode_attend_score, L.voxzip_evict_compact, L.voxzip_decode_evict,
-              L.voxzip_fuse_spans_ragged, L.voxzip_decode_attend_score_ragged, L.voxzip_evict_compact_ragged):
+              L.voxzip_fuse_spans_ragged, L.voxzip_decode_attend_score_ragged, L.voxzip_evict_compact_ragged,
+              L.voxzip_fuse_spans_q4, L.voxzip_unpack_q4, L.voxzip_decode_attend_score_q4, L.voxzip_evict_compact_q4,
+              L.voxzip_decode_evict_q4, L.voxzip_fuse_spans_q4_ragged, L.voxzip_decode_attend_score_q4_ragged,
+              L.voxzip_evict_compact_q4_ragged):
         f.restype = ctypes.c_int
     L.voxzip_status_string.argtypes = [ctypes.c_int]
     L.voxzip_status_string.restype = ctypes.c_char_p
@@ -361,3 +379,184 @@ def voxzip_evict_compact_ragged(k_cache, v_cache, score, pos, seq_base, cap, len
         None if new_len_out is None else _seq_array(new_len_out, n, "int32", "new_len_out"),
         None if status is None else _seq_array(status, n, "int32", "status"), L, Hkv, d, _dtype_code(k_cache),
         _ptr(workspace), ws_bytes, _stream(stream)))
+
+
+# ---- 4-bit caches: codes uint8 [L][H][cap][d / 2] and scales uint8 [L][H][cap][d / 32] for K and for V ----
+
+def q4_cache(n_layers: int, kv_heads: int, cap: int, d: int, device="cuda"):
+    """A zero-filled 4-bit cache: (k_codes, k_scales, v_codes, v_scales), the
+    order in which the ``*_q4`` functions take them."""
+    import torch
+    plane = lambda n: torch.zeros(n_layers, kv_heads, cap, n, dtype=torch.uint8, device=device)
+    return plane(d // 2), plane(d // 32), plane(d // 2), plane(d // 32)
+
+
+def _expect_q4(d, k_codes, k_scales, v_codes, v_scales):
+    """Checks a 4-bit cache of head size d and returns (L, H, slots)."""
+    import torch
+    if d not in (64, 128):
+        raise ValueError(f"head size must be 64 or 128, not {d}")
+    if k_codes.dim() != 4:
+        raise ValueError("k_codes must be [layers][heads][slots][d / 2]")
+    L, H, cap = k_codes.shape[:3]
+    u8, codes, scales = torch.uint8, (L, H, cap, d // 2), (L, H, cap, d // 32)
+    _expect_all(((k_codes, codes, "k_codes", u8), (k_scales, scales, "k_scales", u8), (v_codes, codes, "v_codes", u8),
+                 (v_scales, scales, "v_scales", u8)))
+    return L, H, cap
+
+
+def voxzip_fuse_spans_q4(k_in, v_in, span_off, k_codes, k_scales, v_codes, v_scales, score_out, pos_out,
+                         anchor_k=None, anchor_v=None, stream=None) -> None:
+    """Stage-1 fusion into a 4-bit cache; k_in/v_in [L][H][T_in][d], span_off
+    int32 [n+1] on the device.  Spans of length 1 pack rows as they are."""
+    import torch
+    L, H, T_in, d = k_in.shape
+    cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)[2]
+    n = span_off.numel() - 1
+    dt, span_shape = k_in.dtype, (L, H, n, d)
+    _expect_all(((k_codes, (L, H, cap, d // 2), "k_codes", None), (v_in, (L, H, T_in, d), "v_in", dt),
+                 (score_out, (L, cap), "score_out", torch.float32), (pos_out, (L, cap), "pos_out", torch.int32),
+                 (span_off, (n + 1,), "span_off", torch.int32), (anchor_k, span_shape, "anchor_k", dt),
+                 (anchor_v, span_shape, "anchor_v", dt)))
+    _check(lib().voxzip_fuse_spans_q4(_ptr(k_in), _ptr(v_in), T_in, _ptr(span_off), n, _ptr(anchor_k),
+                                      _ptr(anchor_v), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales),
+                                      _ptr(score_out), _ptr(pos_out), L, H, d, cap, _dtype_code(k_in),
+                                      _stream(stream)))
+
+
+def voxzip_unpack_q4(codes, scales, out, stream=None) -> None:
+    """The values of 4-bit rows: codes [..., d / 2] and scales [..., d / 32]
+    into out [..., d] (float32 or bfloat16)."""
+    import torch
+    d = out.shape[-1]
+    rows = tuple(out.shape[:-1])
+    _expect_all(((codes, rows + (d // 2,), "codes", torch.uint8), (scales, rows + (d // 32,), "scales", torch.uint8)))
+    n = out.numel() // d if d else 0
+    if n == 0:
+        return
+    _check(lib().voxzip_unpack_q4(_ptr(codes), _ptr(scales), n, d, _ptr(out), _dtype_code(out), _stream(stream)))
+
+
+def voxzip_decode_attend_score_q4(q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out, length,
+                                  next_pos, gamma, sm_scale=0.0, workspace=None, stream=None) -> None:
+    """One decode step over all layers of a 4-bit cache; q/out [L][Hq][d]."""
+    import torch
+    Hq, d = q.shape[1:]
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    dt = q.dtype
+    rows, new_rows, plane = (L, Hq, d), (L, Hkv, d), (L, cap)
+    _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
+                 (v_new, new_rows, "v_new", dt), (score, plane, "score", torch.float32),
+                 (pos, plane, "pos", torch.int32)))
+    _check(lib().voxzip_decode_attend_score_q4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_codes), _ptr(k_scales),
+                                               _ptr(v_codes), _ptr(v_scales), _ptr(score), _ptr(pos), _ptr(out),
+                                               int(length), int(next_pos), float(gamma), float(sm_scale), L, Hq, Hkv,
+                                               d, cap, _dtype_code(q), _ptr(workspace), _nbytes(workspace),
+                                               _stream(stream)))
+
+
+def voxzip_evict_compact_q4(k_codes, k_scales, v_codes, v_scales, score, pos, length, budget, next_pos, n_sink=4,
+                            n_recent=-1, kept_pos_out=None, workspace=None, stream=None) -> int:
+    """Stage-2 eviction of a 4-bit cache, in place; returns the new resident length."""
+    import torch
+    d = 2 * k_codes.shape[-1]
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    _expect_all(((score, (L, cap), "score", torch.float32), (pos, (L, cap), "pos", torch.int32),
+                 (kept_pos_out, (L, int(budget)), "kept_pos_out", torch.int32)))
+    new_len = ctypes.c_int32(0)
+    _check(lib().voxzip_evict_compact_q4(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score),
+                                         _ptr(pos), int(length), int(budget), int(n_sink), int(n_recent),
+                                         int(next_pos), _ptr(kept_pos_out), ctypes.byref(new_len), L, Hkv, d, cap,
+                                         _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    return int(new_len.value)
+
+
+def voxzip_decode_evict_q4(q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out, length, next_pos,
+                           gamma, budget, n_sink=4, n_recent=-1, kept_pos_out=None, sm_scale=0.0, workspace=None,
+                           stream=None) -> int:
+    """One generation step over a 4-bit cache: the decode step at (length,
+    next_pos), then the eviction of the length + 1 slots it leaves; returns the
+    new resident length."""
+    import torch
+    Hq, d = q.shape[1:]
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    dt = q.dtype
+    rows, new_rows, plane = (L, Hq, d), (L, Hkv, d), (L, cap)
+    _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
+                 (v_new, new_rows, "v_new", dt), (score, plane, "score", torch.float32),
+                 (pos, plane, "pos", torch.int32), (kept_pos_out, (L, int(budget)), "kept_pos_out", torch.int32)))
+    new_len = ctypes.c_int32(0)
+    _check(lib().voxzip_decode_evict_q4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_codes), _ptr(k_scales),
+                                        _ptr(v_codes), _ptr(v_scales), _ptr(score), _ptr(pos), _ptr(out), int(length),
+                                        int(next_pos), float(gamma), float(sm_scale), int(budget), int(n_sink),
+                                        int(n_recent), _ptr(kept_pos_out), ctypes.byref(new_len), L, Hq, Hkv, d, cap,
+                                        _dtype_code(q), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    return int(new_len.value)
+
+
+def voxzip_fuse_spans_q4_ragged(k_in, v_in, in_base, T_in, span_off, off_base, n_spans, max_spans: int, k_codes,
+                                k_scales, v_codes, v_scales, score_out, pos_out, seq_base, cap, status=None,
+                                anchor_k=None, anchor_v=None, stream=None) -> None:
+    """Stage-1 fusion of every sequence of a ragged batch into a packed 4-bit
+    cache; k_in/v_in [L][H][total_in][d], anchors [L][H][total][d]."""
+    import torch
+    L, H, total_in, d = k_in.shape
+    total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)[2]
+    n = seq_base.numel()
+    dt, out_shape = k_in.dtype, (L, H, total, d)
+    if span_off.dtype != torch.int32 or span_off.dim() != 1:
+        raise TypeError("span_off must be a 1-D int32 tensor")
+    _expect_all(((k_codes, (L, H, total, d // 2), "k_codes", None), (v_in, (L, H, total_in, d), "v_in", dt),
+                 (score_out, (L, total), "score_out", torch.float32), (pos_out, (L, total), "pos_out", torch.int32),
+                 (anchor_k, out_shape, "anchor_k", dt), (anchor_v, out_shape, "anchor_v", dt)))
+    _check(lib().voxzip_fuse_spans_q4_ragged(
+        _ptr(k_in), _ptr(v_in), _seq_array(in_base, n, "int64", "in_base"), _seq_array(T_in, n, "int32", "T_in"),
+        total_in, _ptr(span_off), _seq_array(off_base, n, "int64", "off_base"),
+        _seq_array(n_spans, n, "int32", "n_spans"), span_off.numel(), int(max_spans), _ptr(anchor_k),
+        _ptr(anchor_v), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score_out), _ptr(pos_out),
+        _seq_array(seq_base, n, "int64", "seq_base"), _seq_array(cap, n, "int32", "cap"), total, n,
+        None if status is None else _seq_array(status, n, "int32", "status"), L, H, d, _dtype_code(k_in),
+        _stream(stream)))
+
+
+def voxzip_decode_attend_score_q4_ragged(q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out,
+                                         seq_base, cap, length, next_pos, gamma, sm_scale=0.0, status=None,
+                                         workspace=None, stream=None) -> None:
+    """One decode step of every sequence of a ragged batch over a packed 4-bit
+    cache; q/out [S][L][Hq][d], k_new/v_new [S][L][Hkv][d]."""
+    import torch
+    n, _, Hq, d = q.shape
+    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    dt = q.dtype
+    rows, new_rows, plane = (n, L, Hq, d), (n, L, Hkv, d), (L, total)
+    _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
+                 (v_new, new_rows, "v_new", dt), (score, plane, "score", torch.float32),
+                 (pos, plane, "pos", torch.int32)))
+    _check(lib().voxzip_decode_attend_score_q4_ragged(
+        _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score),
+        _ptr(pos), _ptr(out), _seq_array(seq_base, n, "int64", "seq_base"), _seq_array(cap, n, "int32", "cap"),
+        _seq_array(length, n, "int32", "length"), _seq_array(next_pos, n, "int32", "next_pos"), total, n,
+        float(gamma), float(sm_scale), L, Hq, Hkv, d, _dtype_code(q),
+        None if status is None else _seq_array(status, n, "int32", "status"), _ptr(workspace), _nbytes(workspace),
+        _stream(stream)))
+
+
+def voxzip_evict_compact_q4_ragged(k_codes, k_scales, v_codes, v_scales, score, pos, seq_base, cap, length, budget,
+                                   next_pos, n_sink=4, n_recent=-1, kept_pos_out=None, new_len_out=None, status=None,
+                                   workspace=None, stream=None) -> None:
+    """Stage-2 eviction of every sequence of a ragged batch in a packed 4-bit
+    cache; new_len_out (int32 [S], device) receives min(length, budget)."""
+    import torch
+    d = 2 * k_codes.shape[-1]
+    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    n, plane = seq_base.numel(), (L, total)
+    _expect_all(((score, plane, "score", torch.float32), (pos, plane, "pos", torch.int32),
+                 (kept_pos_out, plane, "kept_pos_out", torch.int32)))
+    _check(lib().voxzip_evict_compact_q4_ragged(
+        _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score), _ptr(pos),
+        _seq_array(seq_base, n, "int64", "seq_base"), _seq_array(cap, n, "int32", "cap"),
+        _seq_array(length, n, "int32", "length"), _seq_array(budget, n, "int32", "budget"),
+        _seq_array(next_pos, n, "int32", "next_pos"), total, n, int(n_sink), int(n_recent), _ptr(kept_pos_out),
+        None if new_len_out is None else _seq_array(new_len_out, n, "int32", "new_len_out"),
+        None if status is None else _seq_array(status, n, "int32", "status"), L, Hkv, d, _ptr(workspace),
+        _nbytes(workspace), _stream(stream)))

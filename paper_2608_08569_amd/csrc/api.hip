@@ -78,6 +78,15 @@ int check_ragged(const char* fn, int32_t L, int32_t Hkv, int32_t d, int32_t dtyp
     return VZ_OK;
 }
 
+// Head counts of a decode step.
+int check_heads(const char* fn, int32_t n_q_heads, int32_t kv_heads) {
+    if (n_q_heads < 1 || n_q_heads % kv_heads != 0)
+        return fail(VZ_ERR_SHAPE, fn, "n_q_heads must be a positive multiple of kv_heads");
+    if (n_q_heads / kv_heads > 16) return fail(VZ_ERR_UNSUPPORTED, fn, "more than 16 query heads per KV head");
+    if (n_q_heads > 256) return fail(VZ_ERR_UNSUPPORTED, fn, "more than 256 query heads");
+    return VZ_OK;
+}
+
 // Arguments of a single-sequence decode step (shared by the decode entry
 // points).
 int check_decode(const char* fn, const void* q, const void* k_new, const void* v_new, const void* k_cache,
@@ -88,10 +97,8 @@ int check_decode(const char* fn, const void* q, const void* k_new, const void* v
         return fail(VZ_ERR_INVALID, fn, "null pointer");
     int rc = check_common(fn, n_layers, kv_heads, d, dtype);
     if (rc) return rc;
-    if (n_q_heads < 1 || n_q_heads % kv_heads != 0)
-        return fail(VZ_ERR_SHAPE, fn, "n_q_heads must be a positive multiple of kv_heads");
-    if (n_q_heads / kv_heads > 16) return fail(VZ_ERR_UNSUPPORTED, fn, "more than 16 query heads per KV head");
-    if (n_q_heads > 256) return fail(VZ_ERR_UNSUPPORTED, fn, "more than 256 query heads");
+    rc = check_heads(fn, n_q_heads, kv_heads);
+    if (rc) return rc;
     if (len < 0 || next_pos < 0) return fail(VZ_ERR_INVALID, fn, "negative len or next_pos");
     if (cap < 1 || len + 1 > cap) return fail(VZ_ERR_CAPACITY, fn, "no free slot for the new token");
     if (!(gamma >= 0.f && gamma <= 1.f)) return fail(VZ_ERR_INVALID, fn, "gamma must be in [0, 1]");
@@ -125,6 +132,42 @@ bool ws_ok(const void* ws, size_t ws_bytes, size_t need) {
 // the next 256-byte boundary.
 size_t decode_evict_split(int32_t L, int32_t Hq, int32_t Hkv, int32_t d, int32_t cap) {
     return (vz_decode_ws_bytes(L, Hq, Hkv, d, cap, 0) + 255) / 256 * 256;
+}
+size_t decode_evict_q4_split(int32_t L, int32_t Hq, int32_t Hkv, int32_t d, int32_t cap) {
+    return (vz_decode_q4_ws_bytes(L, Hq, Hkv, d, cap, 0) + 255) / 256 * 256;
+}
+
+VzQ4Cache q4_cache(void* kc, void* ks, void* vc, void* vs) {
+    return VzQ4Cache{static_cast<uint8_t*>(kc), static_cast<uint8_t*>(ks), static_cast<uint8_t*>(vc),
+                     static_cast<uint8_t*>(vs)};
+}
+
+constexpr int64_t kUnpackMaxRows = int64_t(1) << 28;
+
+// The planes of a 4-bit cache: present, codes on 16-byte boundaries and scales
+// on a row's (the kernels' accesses).
+int check_q4(const char* fn, const VzQ4Cache& c, int32_t d) {
+    if (!c.kc || !c.ks || !c.vc || !c.vs) return fail(VZ_ERR_INVALID, fn, "null pointer");
+    const uintptr_t codes = reinterpret_cast<uintptr_t>(c.kc) | reinterpret_cast<uintptr_t>(c.vc);
+    const uintptr_t scales = reinterpret_cast<uintptr_t>(c.ks) | reinterpret_cast<uintptr_t>(c.vs);
+    if ((codes & 15u) != 0 || (scales & static_cast<uintptr_t>(d / 32 - 1)) != 0)
+        return fail(VZ_ERR_INVALID, fn, "codes must be 16-byte aligned and scales aligned to a row's d / 32 bytes");
+    return VZ_OK;
+}
+
+// Outputs of a fusion into a 4-bit cache: apart from the inputs and from each other.
+int check_q4_outputs(const char* fn, const VzQ4Cache& c, int64_t rows, int32_t d, const void* k_in, const void* v_in,
+                     size_t in_bytes) {
+    const size_t codes = static_cast<size_t>(rows) * (d / 2), scales = static_cast<size_t>(rows) * (d / 32);
+    const void* outs[4] = {c.kc, c.vc, c.ks, c.vs};
+    const size_t sizes[4] = {codes, codes, scales, scales};
+    for (int i = 0; i < 4; ++i) {
+        if (in_bytes && (overlaps(outs[i], sizes[i], k_in, in_bytes) || overlaps(outs[i], sizes[i], v_in, in_bytes)))
+            return fail(VZ_ERR_INVALID, fn, "an input aliases an output");
+        for (int j = 0; j < i; ++j)
+            if (overlaps(outs[i], sizes[i], outs[j], sizes[j])) return fail(VZ_ERR_INVALID, fn, "outputs overlap");
+    }
+    return VZ_OK;
 }
 
 }  // namespace
@@ -161,6 +204,14 @@ size_t voxzip_workspace_bytes(int32_t op, int32_t n_layers, int32_t n_q_heads, i
         if (n_q_heads < 1) return 0;
         return decode_evict_split(n_layers, n_q_heads, kv_heads, d, cap) + vz_evict_ws_bytes(n_layers, cap, 0);
     }
+    if (op == VZ_OP_DECODE_Q4) {
+        if (n_q_heads < 1) return 0;
+        return vz_decode_q4_ws_bytes(n_layers, n_q_heads, kv_heads, d, cap, 0);
+    }
+    if (op == VZ_OP_DECODE_EVICT_Q4) {
+        if (n_q_heads < 1) return 0;
+        return decode_evict_q4_split(n_layers, n_q_heads, kv_heads, d, cap) + vz_evict_ws_bytes(n_layers, cap, 0);
+    }
     return 0;
 }
 
@@ -173,6 +224,10 @@ size_t voxzip_workspace_bytes_ragged(int32_t op, int32_t n_layers, int32_t n_q_h
         return vz_decode_ws_bytes(n_layers, n_q_heads, kv_heads, d, total, n_seqs);
     }
     if (op == VZ_OP_EVICT) return vz_evict_ws_bytes(n_layers, total, n_seqs);
+    if (op == VZ_OP_DECODE_Q4) {
+        if (n_q_heads < 1) return 0;
+        return vz_decode_q4_ws_bytes(n_layers, n_q_heads, kv_heads, d, total, n_seqs);
+    }
     return 0;
 }
 
@@ -442,10 +497,8 @@ int voxzip_decode_attend_score_ragged(const void* q, const void* k_new, const vo
         return fail(VZ_ERR_INVALID, fn, "null pointer");
     int rc = check_ragged(fn, n_layers, kv_heads, d, dtype, total, n_seqs);
     if (rc) return rc;
-    if (n_q_heads < 1 || n_q_heads % kv_heads != 0)
-        return fail(VZ_ERR_SHAPE, fn, "n_q_heads must be a positive multiple of kv_heads");
-    if (n_q_heads / kv_heads > 16) return fail(VZ_ERR_UNSUPPORTED, fn, "more than 16 query heads per KV head");
-    if (n_q_heads > 256) return fail(VZ_ERR_UNSUPPORTED, fn, "more than 256 query heads");
+    rc = check_heads(fn, n_q_heads, kv_heads);
+    if (rc) return rc;
     if (!(gamma >= 0.f && gamma <= 1.f)) return fail(VZ_ERR_INVALID, fn, "gamma must be in [0, 1]");
     if (!isfinite(sm_scale)) return fail(VZ_ERR_INVALID, fn, "sm_scale must be finite");
     const size_t need = vz_decode_ws_bytes(n_layers, n_q_heads, kv_heads, d, total, n_seqs);
@@ -478,6 +531,224 @@ int voxzip_evict_compact_ragged(void* k_cache, void* v_cache, float* score, int3
     VzEvictArgs a{k_cache, v_cache, score, pos, 0, 0, n_sink, n_recent, 0, kept_pos_out,
                   n_layers, kv_heads, d, 0, dtype, workspace, ws_bytes, rg, new_len_out};
     hipError_t e = vz_launch_evict(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
+}
+
+// ---- 4-bit caches ----
+
+int voxzip_fuse_spans_q4(const void* k_in, const void* v_in, int32_t T_in, const int32_t* span_off, int32_t n_spans,
+                         const void* anchor_k, const void* anchor_v, void* k_codes, void* k_scales, void* v_codes,
+                         void* v_scales, float* score_out, int32_t* pos_out, int32_t n_layers, int32_t kv_heads,
+                         int32_t d, int32_t cap_out, int32_t dtype, void* stream) {
+    static const char* fn = "voxzip_fuse_spans_q4";
+    if (!k_in || !v_in || !span_off || !score_out || !pos_out) return fail(VZ_ERR_INVALID, fn, "null pointer");
+    if ((anchor_k == nullptr) != (anchor_v == nullptr))
+        return fail(VZ_ERR_INVALID, fn, "anchor_k and anchor_v must both be given or both be NULL");
+    int rc = check_common(fn, n_layers, kv_heads, d, dtype);
+    if (rc) return rc;
+    const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
+    rc = check_q4(fn, c, d);
+    if (rc) return rc;
+    if (2 * static_cast<int64_t>(kv_heads) > 65535) return fail(VZ_ERR_UNSUPPORTED, fn, "too many KV heads");
+    if (T_in < 0 || n_spans < 0 || cap_out < 1) return fail(VZ_ERR_SHAPE, fn, "negative size");
+    if (n_spans > T_in) return fail(VZ_ERR_SHAPE, fn, "more spans than input tokens");
+    if (n_spans > cap_out) return fail(VZ_ERR_CAPACITY, fn, "n_spans exceeds cap_out");
+    const int64_t planes = static_cast<int64_t>(n_layers) * kv_heads;
+    rc = check_q4_outputs(fn, c, planes * cap_out, d, k_in, v_in,
+                          static_cast<size_t>(planes) * T_in * d * elem_size(dtype));
+    if (rc) return rc;
+    hipError_t e = vz_launch_fuse_q4(k_in, v_in, T_in, span_off, n_spans, anchor_k, anchor_v, c, score_out, pos_out,
+                                     n_layers, kv_heads, d, cap_out, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
+}
+
+int voxzip_unpack_q4(const void* codes, const void* scales, int64_t n_rows, int32_t d, void* out, int32_t dtype,
+                     void* stream) {
+    static const char* fn = "voxzip_unpack_q4";
+    if (!codes || !scales || !out) return fail(VZ_ERR_INVALID, fn, "null pointer");
+    int rc = check_common(fn, 1, 1, d, dtype);
+    if (rc) return rc;
+    if (n_rows < 0 || n_rows > kUnpackMaxRows) return fail(VZ_ERR_SHAPE, fn, "n_rows must be in [0, 2^28]");
+    if ((reinterpret_cast<uintptr_t>(codes) & 3u) != 0 || (reinterpret_cast<uintptr_t>(out) & 15u) != 0)
+        return fail(VZ_ERR_INVALID, fn, "codes must be 4-byte and out 16-byte aligned");
+    const size_t rows = static_cast<size_t>(n_rows), out_bytes = rows * d * elem_size(dtype);
+    if (rows && (overlaps(codes, rows * (d / 2), out, out_bytes) || overlaps(scales, rows * (d / 32), out, out_bytes)))
+        return fail(VZ_ERR_INVALID, fn, "an input aliases the output");
+    hipError_t e = vz_launch_unpack_q4(static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), n_rows, d,
+                                       out, dtype, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
+}
+
+int voxzip_decode_attend_score_q4(const void* q, const void* k_new, const void* v_new, void* k_codes, void* k_scales,
+                                  void* v_codes, void* v_scales, float* score, int32_t* pos, void* out, int32_t len,
+                                  int32_t next_pos, float gamma, float sm_scale, int32_t n_layers, int32_t n_q_heads,
+                                  int32_t kv_heads, int32_t d, int32_t cap, int32_t dtype, void* workspace,
+                                  size_t ws_bytes, void* stream) {
+    static const char* fn = "voxzip_decode_attend_score_q4";
+    int rc = check_decode(fn, q, k_new, v_new, k_codes, v_codes, score, pos, out, len, next_pos, gamma, sm_scale,
+                          n_layers, n_q_heads, kv_heads, d, cap, dtype);
+    if (rc) return rc;
+    const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
+    rc = check_q4(fn, c, d);
+    if (rc) return rc;
+    const size_t need = vz_decode_q4_ws_bytes(n_layers, n_q_heads, kv_heads, d, cap, 0);
+    if (!ws_ok(workspace, ws_bytes, need)) return fail(VZ_ERR_WORKSPACE, fn, "workspace missing, misaligned or too small");
+    VzDecodeArgs a{q, k_new, v_new, nullptr, nullptr, score, pos, out, len, next_pos, gamma, sm_scale,
+                   n_layers, n_q_heads, kv_heads, d, cap, dtype, workspace, ws_bytes, VzRagged{},
+                   0, 0, 0, 0, nullptr, nullptr};
+    hipError_t e = vz_launch_decode_q4(a, c, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
+}
+
+int voxzip_evict_compact_q4(void* k_codes, void* k_scales, void* v_codes, void* v_scales, float* score, int32_t* pos,
+                            int32_t len, int32_t budget, int32_t n_sink, int32_t n_recent, int32_t next_pos,
+                            int32_t* kept_pos_out, int32_t* new_len_out, int32_t n_layers, int32_t kv_heads, int32_t d,
+                            int32_t cap, void* workspace, size_t ws_bytes, void* stream) {
+    static const char* fn = "voxzip_evict_compact_q4";
+    if (!score || !pos || !new_len_out) return fail(VZ_ERR_INVALID, fn, "null pointer");
+    int rc = check_common(fn, n_layers, kv_heads, d, VZ_BF16);
+    if (rc) return rc;
+    const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
+    rc = check_q4(fn, c, d);
+    if (rc) return rc;
+    int32_t M = 0;
+    rc = check_evict(fn, len, budget, n_sink, n_recent, next_pos, kept_pos_out, cap, M);
+    if (rc) return rc;
+    const bool work = len > budget || kept_pos_out != nullptr;
+    if (work && !ws_ok(workspace, ws_bytes, vz_evict_ws_bytes(n_layers, cap, 0)))
+        return fail(VZ_ERR_WORKSPACE, fn, "workspace missing, misaligned or too small");
+    *new_len_out = len < budget ? len : budget;
+    if (!work) return VZ_OK;
+    VzEvictArgs a{nullptr, nullptr, score, pos, len, budget, n_sink, M, next_pos, kept_pos_out,
+                  n_layers, kv_heads, d, cap, VZ_BF16, workspace, ws_bytes, VzRagged{}, nullptr};
+    hipError_t e = vz_launch_evict_q4(a, c, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
+}
+
+int voxzip_decode_evict_q4(const void* q, const void* k_new, const void* v_new, void* k_codes, void* k_scales,
+                           void* v_codes, void* v_scales, float* score, int32_t* pos, void* out, int32_t len,
+                           int32_t next_pos, float gamma, float sm_scale, int32_t budget, int32_t n_sink,
+                           int32_t n_recent, int32_t* kept_pos_out, int32_t* new_len_out, int32_t n_layers,
+                           int32_t n_q_heads, int32_t kv_heads, int32_t d, int32_t cap, int32_t dtype, void* workspace,
+                           size_t ws_bytes, void* stream) {
+    static const char* fn = "voxzip_decode_evict_q4";
+    int32_t M = 0;
+    size_t need = 0;
+    int rc = check_step(fn, q, k_new, v_new, k_codes, v_codes, score, pos, out, len, next_pos, gamma, sm_scale, budget,
+                        n_sink, n_recent, kept_pos_out, new_len_out, n_layers, n_q_heads, kv_heads, d, cap, dtype, M,
+                        need);
+    if (rc) return rc;
+    const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
+    rc = check_q4(fn, c, d);
+    if (rc) return rc;
+    const size_t split = decode_evict_q4_split(n_layers, n_q_heads, kv_heads, d, cap);
+    need = split + vz_evict_ws_bytes(n_layers, cap, 0);
+    if (!ws_ok(workspace, ws_bytes, need)) return fail(VZ_ERR_WORKSPACE, fn, "workspace missing, misaligned or too small");
+    const int32_t T = len + 1;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    VzDecodeArgs da{q, k_new, v_new, nullptr, nullptr, score, pos, out, len, next_pos, gamma, sm_scale,
+                    n_layers, n_q_heads, kv_heads, d, cap, dtype, workspace, split, VzRagged{},
+                    0, 0, 0, 0, nullptr, nullptr};
+    hipError_t e = vz_launch_decode_q4(da, c, st);
+    if (e == hipSuccess && (T > budget || kept_pos_out != nullptr)) {
+        VzEvictArgs ea{nullptr, nullptr, score, pos, T, budget, n_sink, M, next_pos + 1, kept_pos_out,
+                       n_layers, kv_heads, d, cap, VZ_BF16, static_cast<uint8_t*>(workspace) + split, ws_bytes - split,
+                       VzRagged{}, nullptr};
+        e = vz_launch_evict_q4(ea, c, st);
+    }
+    if (e != hipSuccess) return hip_fail(fn, e);
+    *new_len_out = T < budget ? T : budget;
+    return VZ_OK;
+}
+
+int voxzip_fuse_spans_q4_ragged(const void* k_in, const void* v_in, const int64_t* in_base, const int32_t* T_in,
+                                int64_t total_in, const int32_t* span_off, const int64_t* off_base,
+                                const int32_t* n_spans, int64_t total_off, int32_t max_spans, const void* anchor_k,
+                                const void* anchor_v, void* k_codes, void* k_scales, void* v_codes, void* v_scales,
+                                float* score_out, int32_t* pos_out, const int64_t* seq_base, const int32_t* cap,
+                                int64_t total, int32_t n_seqs, int32_t* status, int32_t n_layers, int32_t kv_heads,
+                                int32_t d, int32_t dtype, void* stream) {
+    static const char* fn = "voxzip_fuse_spans_q4_ragged";
+    if (!k_in || !v_in || !in_base || !T_in || !span_off || !off_base || !n_spans || !score_out || !pos_out ||
+        !seq_base || !cap)
+        return fail(VZ_ERR_INVALID, fn, "null pointer");
+    if ((anchor_k == nullptr) != (anchor_v == nullptr))
+        return fail(VZ_ERR_INVALID, fn, "anchor_k and anchor_v must both be given or both be NULL");
+    int rc = check_ragged(fn, n_layers, kv_heads, d, dtype, total, n_seqs);
+    if (rc) return rc;
+    const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
+    rc = check_q4(fn, c, d);
+    if (rc) return rc;
+    if (total_in < 0 || total_off < 1 || max_spans < 0) return fail(VZ_ERR_SHAPE, fn, "negative size");
+    if (total_in > kRaggedMaxTotal || max_spans > total) return fail(VZ_ERR_SHAPE, fn, "size out of range");
+    if (2 * static_cast<int64_t>(kv_heads) > 65535) return fail(VZ_ERR_UNSUPPORTED, fn, "too many KV heads");
+    // a block of 256 threads takes at least 8 spans: fewer than 2^32 threads
+    if ((static_cast<int64_t>(max_spans) / 8 + 1) * n_seqs >= (int64_t(1) << 24))
+        return fail(VZ_ERR_UNSUPPORTED, fn, "max_spans x n_seqs too large");
+    const int64_t planes = static_cast<int64_t>(n_layers) * kv_heads;
+    rc = check_q4_outputs(fn, c, planes * total, d, k_in, v_in,
+                          static_cast<size_t>(planes) * total_in * d * elem_size(dtype));
+    if (rc) return rc;
+    VzFuseRaggedArgs a{k_in,     v_in,     in_base,   T_in,      span_off, off_base, n_spans, anchor_k,
+                       anchor_v, nullptr,  nullptr,   score_out, pos_out,  seq_base, cap,     status,
+                       n_seqs,   total_in, total_off, total,     max_spans, n_layers, kv_heads, d,
+                       dtype};
+    hipError_t e = vz_launch_fuse_q4_ragged(a, c, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
+}
+
+int voxzip_decode_attend_score_q4_ragged(const void* q, const void* k_new, const void* v_new, void* k_codes,
+                                         void* k_scales, void* v_codes, void* v_scales, float* score, int32_t* pos,
+                                         void* out, const int64_t* seq_base, const int32_t* cap, const int32_t* len,
+                                         const int32_t* next_pos, int64_t total, int32_t n_seqs, float gamma,
+                                         float sm_scale, int32_t n_layers, int32_t n_q_heads, int32_t kv_heads,
+                                         int32_t d, int32_t dtype, int32_t* status, void* workspace, size_t ws_bytes,
+                                         void* stream) {
+    static const char* fn = "voxzip_decode_attend_score_q4_ragged";
+    if (!q || !k_new || !v_new || !score || !pos || !out || !seq_base || !cap || !len || !next_pos)
+        return fail(VZ_ERR_INVALID, fn, "null pointer");
+    int rc = check_ragged(fn, n_layers, kv_heads, d, dtype, total, n_seqs);
+    if (rc) return rc;
+    const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
+    rc = check_q4(fn, c, d);
+    if (rc) return rc;
+    rc = check_heads(fn, n_q_heads, kv_heads);
+    if (rc) return rc;
+    if (!(gamma >= 0.f && gamma <= 1.f)) return fail(VZ_ERR_INVALID, fn, "gamma must be in [0, 1]");
+    if (!isfinite(sm_scale)) return fail(VZ_ERR_INVALID, fn, "sm_scale must be finite");
+    const size_t need = vz_decode_q4_ws_bytes(n_layers, n_q_heads, kv_heads, d, total, n_seqs);
+    if (!ws_ok(workspace, ws_bytes, need)) return fail(VZ_ERR_WORKSPACE, fn, "workspace missing, misaligned or too small");
+    VzRagged rg{seq_base, cap, len, next_pos, nullptr, status, n_seqs, total};
+    VzDecodeArgs a{q, k_new, v_new, nullptr, nullptr, score, pos, out, 0, 0, gamma, sm_scale,
+                   n_layers, n_q_heads, kv_heads, d, 0, dtype, workspace, ws_bytes, rg,
+                   0, 0, 0, 0, nullptr, nullptr};
+    hipError_t e = vz_launch_decode_q4(a, c, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
+}
+
+int voxzip_evict_compact_q4_ragged(void* k_codes, void* k_scales, void* v_codes, void* v_scales, float* score,
+                                   int32_t* pos, const int64_t* seq_base, const int32_t* cap, const int32_t* len,
+                                   const int32_t* budget, const int32_t* next_pos, int64_t total, int32_t n_seqs,
+                                   int32_t n_sink, int32_t n_recent, int32_t* kept_pos_out, int32_t* new_len_out,
+                                   int32_t* status, int32_t n_layers, int32_t kv_heads, int32_t d, void* workspace,
+                                   size_t ws_bytes, void* stream) {
+    static const char* fn = "voxzip_evict_compact_q4_ragged";
+    if (!score || !pos || !seq_base || !cap || !len || !budget || !next_pos)
+        return fail(VZ_ERR_INVALID, fn, "null pointer");
+    int rc = check_ragged(fn, n_layers, kv_heads, d, VZ_BF16, total, n_seqs);
+    if (rc) return rc;
+    const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
+    rc = check_q4(fn, c, d);
+    if (rc) return rc;
+    if (n_sink < 0) return fail(VZ_ERR_INVALID, fn, "n_sink must be >= 0");
+    if (new_len_out && overlaps(new_len_out, 4 * static_cast<size_t>(n_seqs), len, 4 * static_cast<size_t>(n_seqs)))
+        return fail(VZ_ERR_INVALID, fn, "new_len_out must not overlap len");
+    const size_t need = vz_evict_ws_bytes(n_layers, total, n_seqs);
+    if (!ws_ok(workspace, ws_bytes, need)) return fail(VZ_ERR_WORKSPACE, fn, "workspace missing, misaligned or too small");
+    VzRagged rg{seq_base, cap, len, next_pos, budget, status, n_seqs, total};
+    VzEvictArgs a{nullptr, nullptr, score, pos, 0, 0, n_sink, n_recent, 0, kept_pos_out,
+                  n_layers, kv_heads, d, 0, VZ_BF16, workspace, ws_bytes, rg, new_len_out};
+    hipError_t e = vz_launch_evict_q4(a, c, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? VZ_OK : hip_fail(fn, e);
 }
 

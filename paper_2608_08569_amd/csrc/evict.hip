@@ -10,20 +10,13 @@
 // 13,186 -> 3,277 slots takes 16 us (36 us with the keys read again from
 // memory for every digit and twice for the classification, and 8-bit digits).
 #include <algorithm>
-#include <type_traits>
 
-#include "select.h"
+#include "evict_args.h"
 
 namespace {
 
 using namespace vz_sel;
-
-constexpr int kSel = 1024;
-constexpr int kLdsSlots = 16384;    // slots whose keys fit in LDS
-static_assert(kLdsSlots % (2 * kSel) == 0, "one load round of the LDS keys");
-
-template <bool LK>
-using SelSh = SelShared<kSel, LK ? kLdsSlots : 0>;
+using namespace vz_evict;
 
 // Single sequence: one block per layer.
 template <int DT, int D, bool LK>
@@ -52,20 +45,6 @@ __global__ __launch_bounds__(kSel) void select_kernel(const VzEvictArgs a, int32
     job.Hkv = a.Hkv;
     job.inline_kv = inline_kv;
     select_body<kSel, DT, D, LK>(job, sh);
-}
-
-// Status of sequence s for an eviction (VZ_OK when it can be served, VZ_IDLE
-// for an idle slot).
-__device__ int ragged_evict_status(const VzRagged& r, int s, int n_sink, int n_recent, bool kept) {
-    const int64_t b = r.base[s];
-    const int c = r.cap[s], n = r.len[s], B = r.budget[s], p = r.next_pos[s];
-    if (c == 0) return VZ_IDLE;
-    if (n < 0 || c < 1 || b < 0 || b > r.total - c) return VZ_ERR_INVALID;
-    if (n > c) return VZ_ERR_CAPACITY;
-    const int M = n_recent < 0 ? B / 5 : n_recent;
-    if (B < 1 || static_cast<int64_t>(n_sink) + M > B || p < n) return VZ_ERR_INVALID;
-    if (kept && p > (1 << 18)) return VZ_ERR_UNSUPPORTED;
-    return VZ_OK;
 }
 
 // Ragged batch: one block per (layer, sequence).  The keys go to LDS when the
@@ -156,19 +135,6 @@ __global__ __launch_bounds__(256) void compact_kernel(const VzEvictArgs a, const
             *reinterpret_cast<const uint4*>(hb + static_cast<size_t>(src[r]) * D);
     }
 }
-
-// Workspace: move counts [jobs rounded up to 64], then source and destination
-// lists [L][plane] each.
-struct EvictWs {
-    int32_t* n;
-    int32_t* src;
-    int32_t* dst;
-    EvictWs(void* ws, int64_t jobs, int32_t L, int64_t plane) {
-        n = static_cast<int32_t*>(ws);
-        src = n + 64 * ((jobs + 63) / 64);
-        dst = src + static_cast<size_t>(L) * plane;
-    }
-};
 
 template <int DT, int D>
 hipError_t launch(const VzEvictArgs& a, hipStream_t stream) {

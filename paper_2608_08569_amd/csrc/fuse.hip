@@ -15,54 +15,11 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "vz_internal.h"
+#include "fuse_args.h"
 
 namespace {
 
-struct FuseArgs {
-    const void* k_in;
-    const void* v_in;
-    const int32_t* off;
-    const void* ak;
-    const void* av;
-    void* k_out;
-    void* v_out;
-    float* score_out;
-    int32_t* pos_out;
-    int32_t H;
-    int32_t kinds;              // 2: K and V, 1: K only
-    int32_t d;                  // row length (the wide-row kernel)
-    int32_t T_in, n_spans;      // single sequence
-    int64_t in_plane, out_plane;  // rows per (layer, head) plane of the input and of the output
-    int32_t blocks_per_seq;     // ragged: span blocks per sequence in grid x
-    // ragged batch (n_seqs > 0): sequence s reads input rows in_base[s] ..
-    // + T_in[s] and offsets off[off_base[s] .. + n_spans[s]], writes output
-    // slots base[s] .. + n_spans[s] (cap[s] slots are its own)
-    int32_t n_seqs;
-    const int64_t* in_base;
-    const int32_t* T_in_s;
-    const int64_t* off_base;
-    const int32_t* n_spans_s;
-    const int64_t* base;
-    const int32_t* cap;
-    int32_t* status;
-    int64_t total_off;
-    int32_t max_spans;
-};
-
-// Status of sequence s of a ragged fusion (VZ_OK when it can be served,
-// VZ_IDLE for an idle slot).
-__device__ int ragged_fuse_status(const FuseArgs& a, int s) {
-    const int64_t ib = a.in_base[s], ob = a.off_base[s], b = a.base[s];
-    const int T = a.T_in_s[s], n = a.n_spans_s[s], c = a.cap[s];
-    if (c == 0) return VZ_IDLE;
-    if (T < 0 || n < 0 || c < 1 || ib < 0 || ib > a.in_plane - T || ob < 0 || ob > a.total_off - n - 1 || b < 0 ||
-        b > a.out_plane - c)
-        return VZ_ERR_INVALID;
-    if (n > T) return VZ_ERR_SHAPE;
-    if (n > c || n > a.max_spans) return VZ_ERR_CAPACITY;
-    return VZ_OK;
-}
+using vz_fuse::FuseArgs;
 
 // Adds rows [b, e) of NC 16-byte columns (gap elements apart) to acc in row
 // order (col: row 0 of the first, stride elements per row), four rows' loads
@@ -329,9 +286,7 @@ hipError_t launch(const FuseArgs& a, int32_t L, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t dispatch(FuseArgs a, int32_t L, int32_t d, int32_t dtype, hipStream_t stream) {
-    a.kinds = a.v_in ? 2 : 1;
-    a.d = d;
+hipError_t dispatch(const FuseArgs& a, int32_t L, int32_t d, int32_t dtype, hipStream_t stream) {
     if (dtype == VZ_BF16 && d == 128) return launch<VZ_BF16, 128>(a, L, stream);
     if (dtype == VZ_BF16 && d == 64) return launch<VZ_BF16, 64>(a, L, stream);
     if (dtype == VZ_F32 && d == 128) return launch<VZ_F32, 128>(a, L, stream);
@@ -347,47 +302,15 @@ hipError_t vz_launch_fuse(const void* k_in, const void* v_in, int32_t T_in, cons
                           int32_t n_spans, const void* ak, const void* av, void* k_out, void* v_out,
                           float* score_out, int32_t* pos_out, int32_t L, int32_t H, int32_t d,
                           int32_t cap_out, int32_t dtype, hipStream_t stream) {
-    FuseArgs a{};
-    a.k_in = k_in;
-    a.v_in = v_in;
-    a.off = off;
-    a.ak = ak;
-    a.av = av;
+    FuseArgs a = vz_fuse::fuse_args(k_in, v_in, T_in, off, n_spans, ak, av, score_out, pos_out, H, d, cap_out);
     a.k_out = k_out;
     a.v_out = v_out;
-    a.score_out = score_out;
-    a.pos_out = pos_out;
-    a.H = H;
-    a.T_in = T_in;
-    a.n_spans = n_spans;
-    a.in_plane = T_in;
-    a.out_plane = cap_out;
     return dispatch(a, L, d, dtype, stream);
 }
 
 hipError_t vz_launch_fuse_ragged(const VzFuseRaggedArgs& g, hipStream_t stream) {
-    FuseArgs a{};
-    a.k_in = g.k_in;
-    a.v_in = g.v_in;
-    a.off = g.span_off;
-    a.ak = g.anchor_k;
-    a.av = g.anchor_v;
+    FuseArgs a = vz_fuse::fuse_args(g);
     a.k_out = g.k_out;
     a.v_out = g.v_out;
-    a.score_out = g.score_out;
-    a.pos_out = g.pos_out;
-    a.H = g.Hkv;
-    a.in_plane = g.total_in;
-    a.out_plane = g.total;
-    a.n_seqs = g.n_seqs;
-    a.in_base = g.in_base;
-    a.T_in_s = g.T_in;
-    a.off_base = g.off_base;
-    a.n_spans_s = g.n_spans;
-    a.base = g.seq_base;
-    a.cap = g.cap;
-    a.status = g.status;
-    a.total_off = g.total_off;
-    a.max_spans = g.max_spans;
     return dispatch(a, g.L, g.d, g.dtype, stream);
 }

@@ -1,0 +1,215 @@
+// Rows into and out of a 4-bit cache.
+//
+// fuse:   Stage-1 fusion (Sec. 3.2.1, Eq. 4-5) whose rows are quantised where
+//         they are formed: x_j = (sum over span j of x_r + n_j a_j) / n_j, then
+//         the block scales and codes of q4.h.  A span of length 1 packs its row
+//         as it stands, so this is also how full-precision rows enter the cache.
+// unpack: the values that codes and scales stand for.
+//
+// A lane group of d / (16 bytes) lanes owns one (layer, KV head, K-or-V, span),
+// each lane 16 contiguous bytes of the row, as in fuse.hip; a block's 32
+// channels lie in 4 (bfloat16) or 8 (float32) neighbouring lanes, whose maximum
+// is two or three DPP steps.  Sums are 64-bit: sums of bfloat16 and float32
+// rows are then exact but for extreme spreads, so a value's code does not turn
+// on the order of the rows, and a mean on a code's border is on it here as in
+// the definition.  gfx950 adds, compares and converts float64 at the float32
+// rate, and the call stays bound by its input.
+#include <algorithm>
+
+#include "fuse_args.h"
+#include "q4.h"
+
+namespace {
+
+using vz_fuse::FuseArgs;
+
+template <int CTRL>
+__device__ __forceinline__ double dpp_f64(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, 0xF, 0xF, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xF, 0xF, false);
+    return __builtin_bit_cast(double, (static_cast<uint64_t>(hi) << 32) | lo);
+}
+constexpr int kSwap1 = 0xB1;        // quad_perm [1, 0, 3, 2]
+constexpr int kSwap2 = 0x4E;        // quad_perm [2, 3, 0, 1]
+constexpr int kHalfMirror = 0x141;  // row_half_mirror: the other quad of eight lanes
+
+template <int DT, int D, bool RAG>
+__global__ __launch_bounds__(256) void fuse_q4_kernel(const FuseArgs a, const VzQ4Cache out) {
+    using E = vz::Elem<DT>;
+    using T = typename E::T;
+    using R = vz_q4::Rows<D>;
+    constexpr int PER = E::kPer16B;              // elements per 16-byte vector
+    constexpr int LANES = D / PER;               // lanes per span row
+    constexpr int SPB = 256 / LANES;             // spans per block
+    constexpr int BLANES = vz_q4::kBlock / PER;  // lanes per block of channels
+    constexpr int ROWS = 4;                      // rows in flight per lane
+
+    const int sub = threadIdx.x / LANES;
+    const int lane = threadIdx.x % LANES;
+    const int which = blockIdx.y & 1;  // 0: K, 1: V
+    const int h = blockIdx.y >> 1;
+    const int l = blockIdx.z;
+    int bx = blockIdx.x, T_in = a.T_in, n_spans = a.n_spans;
+    int64_t in_row = 0, out_row = 0;  // first row of the sequence in its planes
+    const int32_t* off = a.off;
+    if constexpr (RAG) {
+        const int s = blockIdx.x / a.blocks_per_seq;
+        bx = blockIdx.x - s * a.blocks_per_seq;
+        const int st = vz_fuse::ragged_fuse_status(a, s);
+        if (a.status && bx == 0 && blockIdx.y == 0 && l == 0 && threadIdx.x == 0) a.status[s] = st;
+        if (st != VZ_OK) return;
+        T_in = a.T_in_s[s];
+        n_spans = a.n_spans_s[s];
+        in_row = a.in_base[s];
+        out_row = a.base[s];
+        off = a.off + a.off_base[s];
+    }
+    const int64_t j = static_cast<int64_t>(bx) * SPB + sub;
+    if (j >= n_spans) return;
+
+    int32_t b = off[j], e = off[j + 1];
+    b = b < 0 ? 0 : (b > T_in ? T_in : b);
+    e = e < b ? b : (e > T_in ? T_in : e);
+
+    const T* src = static_cast<const T*>(which ? a.v_in : a.k_in) +
+                   ((static_cast<size_t>(l) * a.H + h) * static_cast<size_t>(a.in_plane) + in_row) * D + lane * PER;
+    double acc[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc[i] = 0.0;
+    // four rows' loads at a time, those past the span reading its last row again and adding nothing
+    for (int32_t r = b; r < e; r += ROWS) {
+        uint4 x[ROWS];
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u)
+            x[u] = *reinterpret_cast<const uint4*>(src + static_cast<size_t>(min(r + u, e - 1)) * D);
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            float f[PER];
+            vz::unpack16<DT>(x[u], f);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) acc[i] += r + u < e ? f[i] : 0.f;
+        }
+    }
+    const double n = max(e - b, 1);
+    const T* anchor = static_cast<const T*>(which ? a.av : a.ak);
+    const size_t orow = (static_cast<size_t>(l) * a.H + h) * static_cast<size_t>(a.out_plane) + out_row + j;
+    if (anchor) {
+        // single sequence: [L][H][n_spans][d]; ragged: laid out like the output
+        const size_t arow = RAG ? orow : (static_cast<size_t>(l) * a.H + h) * static_cast<size_t>(n_spans) + j;
+        const uint4 x = *reinterpret_cast<const uint4*>(anchor + arow * D + lane * PER);
+        float f[PER];
+        vz::unpack16<DT>(x, f);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) acc[i] = __builtin_fma(n, f[i], acc[i]);
+    }
+    double top = 0.0;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const double x = __builtin_fabs(acc[i]);
+        bad = bad || !(x < INFINITY);
+        top = __builtin_fmax(top, x);
+    }
+    top = bad ? INFINITY : top;
+    top = __builtin_fmax(top, dpp_f64<kSwap1>(top));
+    top = __builtin_fmax(top, dpp_f64<kSwap2>(top));
+    if constexpr (BLANES == 8) top = __builtin_fmax(top, dpp_f64<kHalfMirror>(top));
+    const vz_q4::Scale s = vz_q4::scale_for(top, n);
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) w |= vz_q4::code_of(acc[i], s.unit) << (4 * i);
+    uint8_t* const codes = (which ? out.vc : out.kc) + orow * R::kCodes;
+    if constexpr (PER == 8) {
+        *reinterpret_cast<uint32_t*>(codes + 4 * lane) = w;
+    } else {  // four codes a lane: the even lane stores its neighbour's too
+        const uint32_t other = __builtin_amdgcn_update_dpp(0, static_cast<int>(w), kSwap1, 0xF, 0xF, false);
+        if ((lane & 1) == 0) *reinterpret_cast<uint32_t*>(codes + 2 * lane) = w | (other << 16);
+    }
+    if (lane % BLANES == 0)
+        ((which ? out.vs : out.ks) + orow * R::kScales)[lane / BLANES] = static_cast<uint8_t>(s.byte);
+
+    if (which == 0 && h == 0 && lane == 0) {
+        const size_t prow = static_cast<size_t>(l) * a.out_plane + out_row + j;
+        a.pos_out[prow] = static_cast<int32_t>(j);
+        a.score_out[prow] = 0.f;
+    }
+}
+
+template <int DT, int D>
+hipError_t launch(FuseArgs a, const VzQ4Cache& out, int32_t L, hipStream_t stream) {
+    constexpr int SPB = 256 / (D / vz::Elem<DT>::kPer16B);
+    if (a.n_seqs > 0) {
+        a.blocks_per_seq = std::max(1, (a.max_spans + SPB - 1) / SPB);  // at least one reports the status
+        const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.blocks_per_seq) * a.n_seqs), 2 * a.H, L);
+        hipLaunchKernelGGL((fuse_q4_kernel<DT, D, true>), grid, dim3(256), 0, stream, a, out);
+        return hipGetLastError();
+    }
+    if (a.n_spans == 0) return hipSuccess;
+    const dim3 grid((a.n_spans + SPB - 1) / SPB, 2 * a.H, L);
+    hipLaunchKernelGGL((fuse_q4_kernel<DT, D, false>), grid, dim3(256), 0, stream, a, out);
+    return hipGetLastError();
+}
+
+hipError_t dispatch(const FuseArgs& a, const VzQ4Cache& out, int32_t L, int32_t d, int32_t dtype, hipStream_t stream) {
+    if (dtype == VZ_BF16 && d == 128) return launch<VZ_BF16, 128>(a, out, L, stream);
+    if (dtype == VZ_BF16 && d == 64) return launch<VZ_BF16, 64>(a, out, L, stream);
+    if (dtype == VZ_F32 && d == 128) return launch<VZ_F32, 128>(a, out, L, stream);
+    if (dtype == VZ_F32 && d == 64) return launch<VZ_F32, 64>(a, out, L, stream);
+    return hipErrorInvalidValue;
+}
+
+// One 16-byte piece of the output per thread and round: eight bfloat16 from a
+// word of codes, or four float32 from half a word.
+constexpr int kUnpackRounds = 4;
+template <int DT>
+__global__ __launch_bounds__(256) void unpack_kernel(const uint8_t* __restrict__ codes,
+                                                     const uint8_t* __restrict__ scales, uint4* __restrict__ out,
+                                                     int64_t n) {
+    constexpr int PER = vz::Elem<DT>::kPer16B;
+    const int64_t i0 = static_cast<int64_t>(blockIdx.x) * (256 * kUnpackRounds) + threadIdx.x;
+#pragma unroll
+    for (int r = 0; r < kUnpackRounds; ++r) {
+        const int64_t i = i0 + r * 256;
+        if (i >= n) return;
+        const float s = __uint_as_float(static_cast<uint32_t>(scales[i / (vz_q4::kBlock / PER)]) << 23);
+        if constexpr (DT == VZ_BF16) {
+            const uint32_t w = reinterpret_cast<const uint32_t*>(codes)[i];
+            out[i] = make_uint4(vz_q4::pair_bf16<0>(w, s), vz_q4::pair_bf16<1>(w, s), vz_q4::pair_bf16<2>(w, s),
+                                vz_q4::pair_bf16<3>(w, s));
+        } else {
+            const uint32_t w = reinterpret_cast<const uint16_t*>(codes)[i];
+            const vz_q4::f32x2_t a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0);
+            const vz_q4::f32x2_t b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+            out[i] = make_uint4(__float_as_uint(a[0]), __float_as_uint(a[1]), __float_as_uint(b[0]),
+                                __float_as_uint(b[1]));
+        }
+    }
+}
+
+}  // namespace
+
+hipError_t vz_launch_fuse_q4(const void* k_in, const void* v_in, int32_t T_in, const int32_t* off, int32_t n_spans,
+                             const void* ak, const void* av, const VzQ4Cache& out, float* score_out, int32_t* pos_out,
+                             int32_t L, int32_t H, int32_t d, int32_t cap_out, int32_t dtype, hipStream_t stream) {
+    const FuseArgs a = vz_fuse::fuse_args(k_in, v_in, T_in, off, n_spans, ak, av, score_out, pos_out, H, d, cap_out);
+    return dispatch(a, out, L, d, dtype, stream);
+}
+
+hipError_t vz_launch_fuse_q4_ragged(const VzFuseRaggedArgs& g, const VzQ4Cache& out, hipStream_t stream) {
+    return dispatch(vz_fuse::fuse_args(g), out, g.L, g.d, g.dtype, stream);
+}
+
+hipError_t vz_launch_unpack_q4(const uint8_t* codes, const uint8_t* scales, int64_t rows, int32_t d, void* out,
+                               int32_t dtype, hipStream_t stream) {
+    const int64_t n = rows * (d / (dtype == VZ_BF16 ? 8 : 4));
+    if (n == 0) return hipSuccess;
+    const dim3 grid(static_cast<unsigned>((n + 256 * kUnpackRounds - 1) / (256 * kUnpackRounds)));
+    if (dtype == VZ_BF16)
+        hipLaunchKernelGGL((unpack_kernel<VZ_BF16>), grid, dim3(256), 0, stream, codes, scales,
+                           static_cast<uint4*>(out), n);
+    else
+        hipLaunchKernelGGL((unpack_kernel<VZ_F32>), grid, dim3(256), 0, stream, codes, scales,
+                           static_cast<uint4*>(out), n);
+    return hipGetLastError();
+}
