@@ -19,15 +19,28 @@
 // key and KV head (d = 128), mostly from the memory-side cache, where keeping
 // eight heads' float32 logits would write and read 64.
 //
-// Operands: a lane holds the codes of d / 4 channels of a key (K, one load) and
-// of d / 16 channels of eight keys (V); v_cvt_scalef32_pk_bf16_fp4 makes exact
-// bfloat16 of them, scale included, and v_perm_b32 pairs the keys of V.  The
-// accumulator layout of K Q^T (a lane: one head, keys 4 (lane / 16) + i of two
-// 16-key tiles) is the operand layout of P V with its eight contraction steps
-// taken in that key order, so p goes from one product into the other in
-// registers.  Queries and p in bfloat16: one part.  float32: three bfloat16
-// parts, which hold 24 bits, and a product for each.  p is rounded to bfloat16
-// for P V in a bfloat16 call only, whose output has no more bits.
+// K Q^T: v_mfma_scale_f32_16x16x128_f8f6f4 takes K's rows as they lie in the
+// cache -- a lane the 16 bytes of a block's codes, its scale byte the
+// instruction's scale operand -- so K is never converted.  The queries are its
+// e2m3 operand (6 bits), in parts: q = sum over i of part_i 2^(s_i), each part
+// the nearest to what the ones before leave, 4 or 5 bits further down.  Four
+// parts (bfloat16 queries) leave less than 2^-18 of a block's largest channel
+// and nothing of channels within 2^-12 of it; six (float32) less than 2^-28.
+// Two parts ride in the head columns that a group of at most 8 heads leaves
+// free, two in the contraction steps that a row of 64 channels leaves free.
+// The instruction adds these products to float32 precision (errors at most
+// 7e-8 of the sum of the products' magnitudes, none while the blocks' scales
+// are within 2^6); with e4m3 queries it does not (up to 2e-4), and takes twice
+// the time (15.9 against 8.8 ns a SIMD; four 16x16x32 bfloat16 ones and the
+// sixteen conversions of K that they need: 65).
+//
+// P V: v_cvt_scalef32_pk_bf16_fp4 makes exact bfloat16 of V's codes, scale
+// included (a lane: d / 16 channels of eight keys), and v_perm_b32 pairs the
+// keys.  The accumulator layout of K Q^T (a lane: one head, keys 4 (lane / 16)
+// + i of two 16-key tiles) is the operand layout of P V with its eight
+// contraction steps taken in that key order, so p goes from one product into
+// the other in registers; in a bfloat16 call rounded to bfloat16, of which its
+// output has no more bits, in a float32 call as three bfloat16 parts (24 bits).
 #include <math.h>
 
 #include <algorithm>
@@ -42,10 +55,15 @@ using vz_q4::bf16x8_t;
 using vz_q4::Rows;
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u32x6 __attribute__((ext_vector_type(6)));
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / vz::kWave;
 constexpr int kUnit = 32;                 // keys per wave and round
+constexpr int kStatsDepth = 4, kValuesDepth = 1;  // units whose loads are in flight per wave
 constexpr int kMinChunkLog2 = 5;          // chunks of 32 ..
 constexpr int kMaxChunkLog2 = 10;         // .. 1024 keys
 constexpr int kHeads = 16;                // head columns of a matrix instruction, and the largest group
@@ -60,6 +78,7 @@ struct Q4Args {
     float* score;
     int32_t* pos;
     void* out;
+    uint32_t* parts;  // the queries as operands, per (sequence, layer, KV head)
     float2* ml;   // max and sum of exp2 per (layer, head, chunk row, share) [L][Hq][nc_max][shares]
     float* part;  // the chunks' outputs [L][nc_max][shares][Hq][D], each over the sequence's sum of exp2
     int32_t len, next_pos, n_chunks;  // single sequence
@@ -153,10 +172,9 @@ __device__ __forceinline__ void parts_of(const float (&x)[8], bf16x8_t (&p)[NP])
         }
 }
 
-template <int D>
-struct KTile {  // a lane's part of 32 keys: key 16 t + lane % 16, channels D / 4 (lane / 16) ..
-    uint32_t w[2][D / 32];
-    uint32_t s[2];
+struct KTile {  // a lane's part of 32 keys: key 16 t + lane % 16, its block of 32 channels (lane / 16) % (D / 32)
+    uint32_t w[2][4];
+    uint32_t s[2];  // the key's scale bytes
 };
 template <int D>
 struct VTile {  // channels D / 16 (lane % 16) .. of keys 4 (lane / 16) + i and 16 further on
@@ -165,23 +183,22 @@ struct VTile {  // channels D / 16 (lane % 16) .. of keys 4 (lane / 16) + i and 
 };
 
 template <int D>
-__device__ __forceinline__ void load_k(KTile<D>& k, const uint8_t* codes, const uint8_t* scales, int k0, int n) {
+__device__ __forceinline__ int block_of_lane() {
+    return (threadIdx.x % vz::kWave >> 4) % (D / vz_q4::kBlock);
+}
+
+template <int D>
+__device__ __forceinline__ void load_k(KTile& k, const uint8_t* codes, const uint8_t* scales, int k0, int n) {
     using R = Rows<D>;
-    const int lane = threadIdx.x % vz::kWave, q4 = lane >> 4, r16 = lane & 15;
+    const int r16 = threadIdx.x & 15;
     const __amdgpu_buffer_rsrc_t rc = keys_of(codes, k0, n, kUnit, R::kCodes);
     const __amdgpu_buffer_rsrc_t rs = keys_of(scales, k0, n, kUnit, R::kScales);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int off = (16 * t + r16) * R::kCodes + D / 8 * q4;
-        if constexpr (D == 128) {
-            const auto y = __builtin_amdgcn_raw_buffer_load_b128(rc, off, 0, 0);
-            __builtin_memcpy(k.w[t], &y, 16);
-            k.s[t] = __builtin_amdgcn_raw_buffer_load_b32(rs, (16 * t + r16) * 4, 0, 0);
-        } else {
-            const auto y = __builtin_amdgcn_raw_buffer_load_b64(rc, off, 0, 0);
-            __builtin_memcpy(k.w[t], &y, 8);
-            k.s[t] = __builtin_amdgcn_raw_buffer_load_b16(rs, (16 * t + r16) * 2, 0, 0);
-        }
+        const auto y = __builtin_amdgcn_raw_buffer_load_b128(rc, (16 * t + r16) * R::kCodes + 16 * block_of_lane<D>(), 0, 0);
+        __builtin_memcpy(k.w[t], &y, 16);
+        if constexpr (D == 128) k.s[t] = __builtin_amdgcn_raw_buffer_load_b32(rs, (16 * t + r16) * 4, 0, 0);
+        else k.s[t] = __builtin_amdgcn_raw_buffer_load_b16(rs, (16 * t + r16) * 2, 0, 0);
     }
 }
 
@@ -212,59 +229,132 @@ __device__ __forceinline__ void load_v(VTile<D>& v, const uint8_t* codes, const 
     }
 }
 
-// The group's queries as operands: lane (q4, r16) holds channels
-// D / 4 q4 + 8 s .. + 7 of head r16 (zero past the group).
-template <int DT, int D>
+// The group's queries in parts, as operands of products with 16 rows of K:
+// lane (q4, r16) holds its block's 32 channels of head r16 (PACK: r16 & 7; zero
+// past the group), of product j the part in slot 2 j + (r16 >> 3) (PACK) or j;
+// rows of 64 channels take twice as many parts a product, the second half of
+// them in lanes q4 = 2, 3.
+template <int DT, int D, bool PACK>
 struct Queries {
-    static constexpr int NP = DT == VZ_F32 ? 3 : 1;
-    bf16x8_t q[D / 32][NP];
+    static constexpr int kParts = DT == VZ_F32 ? 6 : 4;
+    static constexpr int kSlots = (PACK ? 2 : 1) * (128 / D);  // parts per product
+    static constexpr int kProducts = (kParts + kSlots - 1) / kSlots;
+    i32x8 q[kProducts];  // 6 words of 6-bit codes
+    int s[kProducts];    // scale bytes
     __device__ __forceinline__ void load(const void* q0, int G) {
         using T = typename vz::Elem<DT>::T;
         const int lane = threadIdx.x % vz::kWave, q4 = lane >> 4, r16 = lane & 15;
-        const T* const row = static_cast<const T*>(q0) + static_cast<size_t>(min(r16, G - 1)) * D + D / 4 * q4;
+        const int h = PACK ? r16 & 7 : r16, slot = (PACK ? r16 >> 3 : 0) + (D == 64 ? q4 >> 1 : 0) * (PACK ? 2 : 1);
+        const T* const row = static_cast<const T*>(q0) + static_cast<size_t>(min(h, G - 1)) * D +
+                             vz_q4::kBlock * block_of_lane<D>();
+        f32x16 lo, hi;      // what is left of the even and odd channels (as the conversion takes them)
+        uint32_t bits = 0;  // of the largest magnitude (a NaN's are above infinity's)
+        constexpr int PER = vz::Elem<DT>::kPer16B;
 #pragma unroll
-        for (int s = 0; s < D / 32; ++s) {
-            float f[8];
+        for (int i = 0; i < 32 / PER; ++i) {
+            uint4 x;
+            __builtin_memcpy(&x, row + PER * i, 16);  // any element alignment
+            float f[PER];
+            vz::unpack16<DT>(x, f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = r16 < G ? vz::Elem<DT>::to_f32(row[8 * s + i]) : 0.f;
-            parts_of<NP>(f, q[s]);
+            for (int e = 0; e < PER; ++e) {
+                (e & 1 ? hi : lo)[(PER * i + e) / 2] = f[e];
+                bits = max(bits, __float_as_uint(f[e]) & 0x7FFFFFFFu);
+            }
+        }
+        const float top = __uint_as_float(bits);
+        const bool bad = bits >= 0x7F800000u;
+        // the first part's scale 2^e: top <= 7 2^e; its error is at most 2^(e - 2), the next one's (at 2^(e - 4))
+        // 2^(e - 7), and 2^-5 of that after each further one
+        int e = __builtin_amdgcn_frexp_expf(top) - (__builtin_amdgcn_frexp_mantf(top) > 0.875f ? 2 : 3);
+        e = min(max(e, -96), 125);  // (every part's scale a normal float)
+#pragma unroll
+        for (int j = 0; j < kProducts; ++j) {
+            q[j] = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
+            s[j] = 0;
+        }
+#pragma unroll
+        for (int p = 0; p < kParts; ++p) {
+            const int ep = e - (p == 0 ? 0 : 5 * p - 1) + 127;
+            const float scale = __uint_as_float(static_cast<uint32_t>(ep) << 23);
+            const u32x6 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(lo, hi, scale);
+            if (p + 1 < kParts) {
+                const f32x32 v = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(c, scale);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    lo[i] -= v[2 * i];
+                    hi[i] -= v[2 * i + 1];
+                }
+            }
+            const bool mine = (kSlots == 1 || p % kSlots == slot) && h < G;
+#pragma unroll
+            for (int i = 0; i < 6; ++i) q[p / kSlots][i] = mine ? static_cast<int>(c[i]) : q[p / kSlots][i];
+            s[p / kSlots] = mine ? (bad ? vz_q4::kNoScale : ep) : s[p / kSlots];
+        }
+    }
+    // to and from the workspace, a word per lane
+    static constexpr int kWords = 7 * kProducts * vz::kWave;
+    __device__ __forceinline__ void store(uint32_t* to) const {
+        to += threadIdx.x % vz::kWave;
+#pragma unroll
+        for (int j = 0; j < kProducts; ++j)
+#pragma unroll
+            for (int i = 0; i < 7; ++i) to[(7 * j + i) * vz::kWave] = i < 6 ? q[j][i] : s[j];
+    }
+    __device__ __forceinline__ void reload(const uint32_t* from) {
+        from += threadIdx.x % vz::kWave;
+#pragma unroll
+        for (int j = 0; j < kProducts; ++j) {
+            q[j] = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 6; ++i) q[j][i] = static_cast<int>(from[(7 * j + i) * vz::kWave]);
+            s[j] = static_cast<int>(from[(7 * j + 6) * vz::kWave]);
         }
     }
 };
-
-// Logits (times log2 e) of 32 keys.  PACK (groups of at most 8 heads): set 0
-// holds head r16 & 7, keys 16 (r16 >> 3) + 4 q4 + i, so that every exp2 serves
-// a key and a head that exist; else set t holds head r16, keys 16 t + 4 q4 + i.
+// The parts of a KV head's queries in the workspace (row: (sequence, layer, KV head)).
 template <int DT, int D, bool PACK>
-__device__ __forceinline__ void logits_of(const KTile<D>& k, const Queries<DT, D>& q, float scale_log2, int k0, int n,
-                                          float (&x)[PACK ? 1 : 2][4]) {
+__device__ __forceinline__ uint32_t* parts_of_query(const Q4Args& a, size_t row) {
+    return a.parts + row * Queries<DT, D, PACK>::kWords;
+}
+
+// Q . K of 32 keys (not yet scaled), -inf for keys at or past n (MASK).  PACK
+// (groups of at most 8 heads): set 0 holds head r16 & 7, keys 16 (r16 >> 3) +
+// 4 q4 + i, so that every exp2 serves a key and a head that exist; else set t
+// holds head r16, keys 16 t + 4 q4 + i.
+template <int DT, int D, bool PACK>
+__device__ __forceinline__ void dots_of(const KTile& k, const Queries<DT, D, PACK>& q, int k0, int n,
+                                        float (&x)[PACK ? 1 : 2][4]) {
     const int lane = threadIdx.x % vz::kWave, q4 = lane >> 4, r16 = lane & 15;
-    const int rot = vz_q4::scale_rot(D / 4 * q4 / vz_q4::kBlock);
     f32x4 acc[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const float s = vz_q4::scale_of(k.s[t], rot);
+        const i32x8 w = {static_cast<int>(k.w[t][0]), static_cast<int>(k.w[t][1]), static_cast<int>(k.w[t][2]),
+                         static_cast<int>(k.w[t][3]), 0, 0, 0, 0};
+        const int s = static_cast<int>(k.s[t] >> (8 * block_of_lane<D>()));  // (the low byte counts)
         acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) {
-            const bf16x8_t a = vz_q4::eight_bf16(k.w[t][j], s);
-#pragma unroll
-            for (int p = Queries<DT, D>::NP - 1; p >= 0; --p)
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q.q[j][p], acc[t], 0, 0, 0);
-        }
+        for (int j = Queries<DT, D, PACK>::kProducts - 1; j >= 0; --j)  // formats: 4 e2m1, 2 e2m3
+            acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, q.q[j], acc[t], 4, 2, 0, s, 0, q.s[j]);
     }
     const int half = PACK ? r16 >> 3 : 0;
 #pragma unroll
     for (int t = 0; t < (PACK ? 1 : 2); ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float y = acc[t][i];
             if constexpr (PACK) {
-                const float second = vz::ror16<8>(acc[1][i]);
-                y = half ? second : y;
+                const float y0 = acc[0][i] + vz::ror16<8>(acc[0][i]), y1 = acc[1][i] + vz::ror16<8>(acc[1][i]);
+                x[t][i] = half ? y1 : y0;
+            } else {
+                x[t][i] = acc[t][i];
             }
-            x[t][i] = k0 + 16 * (t + half) + 4 * q4 + i < n ? y * scale_log2 : -INFINITY;
         }
+    if (k0 + kUnit > n) {
+#pragma unroll
+        for (int t = 0; t < (PACK ? 1 : 2); ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[t][i] = k0 + 16 * (t + half) + 4 * q4 + i < n ? x[t][i] : -INFINITY;
+    }
 }
 
 // Eq. (1) for one KV head, by one wave: the new K and V rows quantised and
@@ -303,7 +393,7 @@ __device__ __forceinline__ void append(const Q4Args& a, size_t new_row, size_t s
 }
 
 template <int DT, int D, bool RAG, bool PACK>
-__global__ __launch_bounds__(kThreads) void stats_kernel(const Q4Args a) {
+__global__ __launch_bounds__(kThreads, 4) void stats_kernel(const Q4Args a) {
     using R = Rows<D>;
     __shared__ __align__(16) uint32_t s_new[kWaves][(R::kCodes + 16) / 4];
     const int l = blockIdx.y;
@@ -316,47 +406,61 @@ __global__ __launch_bounds__(kThreads) void stats_kernel(const Q4Args a) {
     const int c0 = c << a.log2_chunk, c1 = min(c0 + (1 << a.log2_chunk), it.len + 1);  // the chunk's keys
     const size_t row_sl = static_cast<size_t>(it.s) * a.L + l;
     const bool newest = it.len < c1 && it.len >= c0;
-    if (newest && threadIdx.x == 0) a.pos[static_cast<size_t>(l) * a.plane + it.base + it.len] = it.next_pos;
-    for (int item = w; item < a.Hkv * shares; item += kWaves) {
+    if (newest && threadIdx.x == 0 && blockIdx.z == 0) a.pos[static_cast<size_t>(l) * a.plane + it.base + it.len] = it.next_pos;
+    const int item = blockIdx.z * kWaves + w;
+    if (item < a.Hkv * shares) {
         const int g = item / shares, share = item - g * shares;
         const size_t head = (static_cast<size_t>(l) * a.Hkv + g) * a.plane + it.base;
         const uint8_t* const kc = a.c.kc + head * R::kCodes;
         const uint8_t* const ks = a.c.ks + head * R::kScales;
         const size_t row_g = row_sl * a.Hkv + g;
-        Queries<DT, D> q;
+        // the wave's units: 32 keys from c0 + 32 (share + shares i) on
+        const int n_units = ((c1 - c0 + kUnit - 1) / kUnit - share + shares - 1) / shares;
+        auto unit_key = [&](int i) { return c0 + kUnit * (share + shares * i); };
+        KTile kt[kStatsDepth];
+        Queries<DT, D, PACK> q;
         q.load(static_cast<const typename vz::Elem<DT>::T*>(a.q) + row_g * G * D, G);
+        if (c == 0 && share == 0) q.store(parts_of_query<DT, D, PACK>(a, row_g));
+        asm volatile("" ::: "memory");  // (the registers of the parts' making are the loads' then)
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < kStatsDepth; ++u) load_k<D>(kt[u], kc, ks, unit_key(u), it.len);
         // the unit that holds the new key, when it is this wave's
         const int u_new = (it.len - c0) / kUnit;
         const bool mine = newest && u_new % shares == share;
         if (mine) append<DT, D>(a, row_g, head + it.len, s_new[w]);
-        float m = -INFINITY, z = 0.f;
-        for (int k0 = c0 + kUnit * share; k0 < c1; k0 += kUnit * shares) {
-            KTile<D> k;
-            load_k<D>(k, kc, ks, k0, it.len);
+        float m = -INFINITY, ref = 0.f, z = 0.f;
+        auto unit = [&](int i, KTile& k) {
+            const int k0 = unit_key(i);
             if (mine && k0 + kUnit > it.len) {
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
                     if (k0 + 16 * t + r16 == it.len) {
 #pragma unroll
-                        for (int j = 0; j < D / 32; ++j) k.w[t][j] = s_new[w][D / 32 * q4 + j];
+                        for (int j = 0; j < 4; ++j) k.w[t][j] = s_new[w][4 * block_of_lane<D>() + j];
                         k.s[t] = s_new[w][R::kCodes / 4];
                     }
             }
             float x[PACK ? 1 : 2][4];
-            logits_of<DT, D, PACK>(k, q, a.scale_log2, k0, c1, x);
-            float mn = m;
+            dots_of<DT, D, PACK>(k, q, k0, c1, x);
+            load_k<D>(k, kc, ks, unit_key(i + kStatsDepth), it.len);  // (past the chunk: nothing)
+            m = fmaxf(m, fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])));
+            if constexpr (!PACK) m = fmaxf(m, fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
+            const float last = ref;
+            ref = finite_ref(m) * a.scale_log2;
+            z *= __builtin_amdgcn_exp2f(last - ref);
 #pragma unroll
             for (int t = 0; t < (PACK ? 1 : 2); ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) mn = fmaxf(mn, x[t][i]);
-            const float ref = finite_ref(mn);
-            z *= __builtin_amdgcn_exp2f(m - ref);
+                for (int e = 0; e < 4; ++e) z += __builtin_amdgcn_exp2f(fmaf(x[t][e], a.scale_log2, -ref));
+        };
+        for (int i = 0; i < n_units; i += kStatsDepth) {
 #pragma unroll
-            for (int t = 0; t < (PACK ? 1 : 2); ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) z += __builtin_amdgcn_exp2f(x[t][i] - ref);
-            m = mn;
+            for (int u = 0; u < kStatsDepth; ++u)
+                if (i + u < n_units) unit(i + u, kt[u]);
         }
+        // the lanes that hold a head: exp2 relative to the largest of their references
+        m = m == -INFINITY ? -INFINITY : ref;
         float mw = vz::rows_max(m);
         if constexpr (PACK) mw = fmaxf(mw, vz::ror16<8>(mw));
         z *= __builtin_amdgcn_exp2f(m - finite_ref(mw));
@@ -410,10 +514,10 @@ __device__ __forceinline__ float2 merge_pairs(const float2* ml, int n) {
 }
 
 template <int DT, int D, bool RAG, bool PACK>
-__global__ __launch_bounds__(kThreads) void values_kernel(const Q4Args a) {
+__global__ __launch_bounds__(kThreads, 3) void values_kernel(const Q4Args a) {
     using R = Rows<D>;
     using E = vz::Elem<DT>;
-    constexpr int NP = Queries<DT, D>::NP;
+    constexpr int NP = DT == VZ_F32 ? 3 : 1;                     // bfloat16 parts of p
     constexpr int NC = D / 16;                                   // channels per lane of V and of an output row
     constexpr int KEYS_PER_THREAD = (1 << kMaxChunkLog2) / kThreads;
     __shared__ float s_sum[kWaves][1 << kMaxChunkLog2];  // per key: the sum of p over a wave's heads
@@ -440,8 +544,17 @@ __global__ __launch_bounds__(kThreads) void values_kernel(const Q4Args a) {
             const uint8_t* const ks = a.c.ks + head * R::kScales;
             const uint8_t* const vc = a.c.vc + head * R::kCodes;
             const uint8_t* const vs = a.c.vs + head * R::kScales;
-            Queries<DT, D> q;
-            q.load(static_cast<const typename E::T*>(a.q) + (row_sl * a.Hkv + g) * G * D, G);
+            const int n_units = ((c1 - c0 + kUnit - 1) / kUnit - share + shares - 1) / shares;
+            auto unit_key = [&](int i) { return c0 + kUnit * (share + shares * i); };
+            KTile kt[kValuesDepth];
+            VTile<D> vt[kValuesDepth];
+            Queries<DT, D, PACK> q;
+            q.reload(parts_of_query<DT, D, PACK>(a, row_sl * a.Hkv + g));
+#pragma unroll
+            for (int u = 0; u < kValuesDepth; ++u) {
+                load_k<D>(kt[u], kc, ks, unit_key(u), c1);
+                load_v<D>(vt[u], vc, vs, unit_key(u), c1);
+            }
             const float2 st = merge_pairs<PACK>(ml_of(a, l, g * G + min(hc, G - 1), it.first), rows);
             // (columns past the group: weights and sums of 0)
             const float ref = hc < G ? finite_ref(st.x) : INFINITY;
@@ -450,20 +563,18 @@ __global__ __launch_bounds__(kThreads) void values_kernel(const Q4Args a) {
 #pragma unroll
             for (int t = 0; t < NC; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
             const int rot = vz_q4::scale_rot(NC * r16 / vz_q4::kBlock);
-            for (int k0 = c0 + kUnit * share; k0 < c1; k0 += kUnit * shares) {
-                KTile<D> k;
-                VTile<D> v;
-                load_k<D>(k, kc, ks, k0, c1);
-                load_v<D>(v, vc, vs, k0, c1);
+            auto unit = [&](int u, KTile& k, VTile<D>& v) {
+                const int k0 = unit_key(u);
                 float x[PACK ? 1 : 2][4];
-                logits_of<DT, D, PACK>(k, q, a.scale_log2, k0, c1, x);
+                dots_of<DT, D, PACK>(k, q, k0, c1, x);
+                load_k<D>(k, kc, ks, unit_key(u + kValuesDepth), c1);  // (past the chunk: nothing)
                 float p[8];
 #pragma unroll
                 for (int t = 0; t < (PACK ? 1 : 2); ++t) {
                     float ks4[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        p[4 * t + i] = __builtin_amdgcn_exp2f(x[t][i] - ref);
+                        p[4 * t + i] = __builtin_amdgcn_exp2f(fmaf(x[t][i], a.scale_log2, -ref));
                         ks4[i] = heads_sum<PACK>(p[4 * t + i] * inv_z);
                     }
                     const float sum = (r16 & 2) ? ((r16 & 1) ? ks4[3] : ks4[2]) : ((r16 & 1) ? ks4[1] : ks4[0]);
@@ -476,33 +587,42 @@ __global__ __launch_bounds__(kThreads) void values_kernel(const Q4Args a) {
                 }
                 bf16x8_t pp[NP];
                 parts_of<NP>(p, pp);
-                // channel pairs of the eight keys, then the keys of a channel side by side
-                uint32_t y[8][NC / 2];
+                // channels 2 b and 2 b + 1 of the eight keys, then the keys of a channel side by side
+                float vs8[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float s = vz_q4::scale_of(v.s[e / 4][e % 4], rot);
-                    const uint32_t wv = v.w[e / 4][e % 4];
-                    y[e][0] = vz_q4::pair_bf16<0>(wv, s);
-                    y[e][1] = vz_q4::pair_bf16<1>(wv, s);
-                    if constexpr (NC == 8) {
-                        y[e][2] = vz_q4::pair_bf16<2>(wv, s);
-                        y[e][3] = vz_q4::pair_bf16<3>(wv, s);
+                for (int e = 0; e < 8; ++e) vs8[e] = vz_q4::scale_of(v.s[e / 4][e % 4], rot);
+                auto channels = [&](auto byte) {
+                    constexpr int B = decltype(byte)::value;
+                    uint32_t y[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[e] = vz_q4::pair_bf16<B>(v.w[e / 4][e % 4], vs8[e]);
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        const uint32_t sel = t ? 0x07060302u : 0x05040100u;  // the high or the low halves of two words
+                        uint4 b;
+                        b.x = __builtin_amdgcn_perm(y[1], y[0], sel);
+                        b.y = __builtin_amdgcn_perm(y[3], y[2], sel);
+                        b.z = __builtin_amdgcn_perm(y[5], y[4], sel);
+                        b.w = __builtin_amdgcn_perm(y[7], y[6], sel);
+                        bf16x8_t vb;
+                        __builtin_memcpy(&vb, &b, 16);
+#pragma unroll
+                        for (int n = NP - 1; n >= 0; --n)
+                            acc[2 * B + t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pp[n], vb, acc[2 * B + t], 0, 0, 0);
                     }
+                };
+                channels(std::integral_constant<int, 0>{});
+                channels(std::integral_constant<int, 1>{});
+                if constexpr (NC == 8) {
+                    channels(std::integral_constant<int, 2>{});
+                    channels(std::integral_constant<int, 3>{});
                 }
+                load_v<D>(v, vc, vs, unit_key(u + kValuesDepth), c1);
+            };
+            for (int i = 0; i < n_units; i += kValuesDepth) {
 #pragma unroll
-                for (int t = 0; t < NC; ++t) {
-                    uint4 b;
-                    const uint32_t sel = t & 1 ? 0x07060302u : 0x05040100u;  // the high or the low halves of two words
-                    b.x = __builtin_amdgcn_perm(y[1][t / 2], y[0][t / 2], sel);
-                    b.y = __builtin_amdgcn_perm(y[3][t / 2], y[2][t / 2], sel);
-                    b.z = __builtin_amdgcn_perm(y[5][t / 2], y[4][t / 2], sel);
-                    b.w = __builtin_amdgcn_perm(y[7][t / 2], y[6][t / 2], sel);
-                    bf16x8_t vb;
-                    __builtin_memcpy(&vb, &b, 16);
-#pragma unroll
-                    for (int n = NP - 1; n >= 0; --n)
-                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pp[n], vb, acc[t], 0, 0, 0);
-                }
+                for (int u = 0; u < kValuesDepth; ++u)
+                    if (i + u < n_units) unit(i + u, kt[u], vt[u]);
             }
             // lane: heads 4 q4 + i, channels NC r16 ..
 #pragma unroll
@@ -571,9 +691,11 @@ __global__ __launch_bounds__(D) void finish_kernel(const Q4Args a) {
         vz::Elem<DT>::from_f32(o);
 }
 
+constexpr int kMostProducts = 6;  // float32, d = 128, groups of more than 8 heads
+
 // Keys per chunk (log2) of a call over `keys` keys per layer: the smallest
 // chunks that leave at most kTargetChunks of them over all layers.
-constexpr int kTargetChunks = 2048, kLeastChunks = 8;
+constexpr int kTargetChunks = 512, kLeastChunks = 8;
 int log2_chunk_for(int32_t L, int64_t keys) {
     const int64_t most = std::max<int64_t>(kLeastChunks, kTargetChunks / L);
     int lg = kMinChunkLog2;
@@ -617,6 +739,8 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
     const size_t rows = static_cast<size_t>(v.L) * a.nc_max * a.shares * v.Hq;
     a.part = static_cast<float*>(v.ws);
     a.ml = reinterpret_cast<float2*>(a.part + rows * D);
+    a.parts = reinterpret_cast<uint32_t*>(a.ml + rows);
+    static_assert(Queries<DT, D, PACK>::kProducts <= kMostProducts, "room in the workspace");
     a.scale_log2 = (v.sm_scale > 0.f ? v.sm_scale : 1.0f / sqrtf(static_cast<float>(D))) * kLog2e;
     a.gamma = v.gamma;
     a.rag = v.rag;
@@ -626,7 +750,7 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
         a.next_pos = v.next_pos;
         a.n_chunks = chunks = (v.len >> a.log2_chunk) + 1;
     }
-    hipLaunchKernelGGL((stats_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((stats_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L, (a.Hkv * a.shares + kWaves - 1) / kWaves), dim3(kThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((values_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L), dim3(kThreads), 0, stream, a);
@@ -647,7 +771,8 @@ hipError_t launch_any(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t str
 
 size_t vz_decode_q4_ws_bytes(int32_t L, int32_t Hq, int32_t Hkv, int32_t d, int64_t plane, int32_t n_seqs) {
     const size_t rows = static_cast<size_t>(L) * chunk_rows(L, plane, n_seqs) * shares_of(Hkv) * Hq;
-    return rows * (d * sizeof(float) + sizeof(float2));
+    const size_t queries = static_cast<size_t>(std::max(n_seqs, 1)) * L * Hkv;
+    return rows * (d * sizeof(float) + sizeof(float2)) + queries * 7 * kMostProducts * vz::kWave * sizeof(uint32_t);
 }
 
 hipError_t vz_launch_decode_q4(const VzDecodeArgs& a, const VzQ4Cache& c, hipStream_t stream) {
