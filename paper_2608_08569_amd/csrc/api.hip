@@ -649,8 +649,15 @@ int voxzip_decode_evict_q4(const void* q, const void* k_new, const void* v_new, 
     VzDecodeArgs da{q, k_new, v_new, nullptr, nullptr, score, pos, out, len, next_pos, gamma, sm_scale,
                     n_layers, n_q_heads, kv_heads, d, cap, dtype, workspace, split, VzRagged{},
                     0, 0, 0, 0, nullptr, nullptr};
+    const bool inside = vz_decode_q4_evicts(da, budget, kept_pos_out != nullptr);
+    if (inside) {
+        da.ev = 1;
+        da.ev_budget = budget;
+        da.ev_sink = n_sink;
+        da.ev_M = M;
+    }
     hipError_t e = vz_launch_decode_q4(da, c, st);
-    if (e == hipSuccess && (T > budget || kept_pos_out != nullptr)) {
+    if (e == hipSuccess && !inside && (T > budget || kept_pos_out != nullptr)) {
         VzEvictArgs ea{nullptr, nullptr, score, pos, T, budget, n_sink, M, next_pos + 1, kept_pos_out,
                        n_layers, kv_heads, d, cap, VZ_BF16, static_cast<uint8_t*>(workspace) + split, ws_bytes - split,
                        VzRagged{}, nullptr};
