@@ -145,7 +145,8 @@ def _nbytes(t) -> int:
 def _stream(stream):
     if stream is None:
         import torch
-        stream = torch.cuda.current_stream()
+        # the current stream's handle without a Stream object (2.7 us of a small call's host time)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     return stream.cuda_stream
 
 
