@@ -23,17 +23,93 @@ namespace {
 
 using vz_fuse::FuseArgs;
 
+constexpr int kSwap1 = 0xB1;        // quad_perm [1, 0, 3, 2]
+constexpr int kSwap2 = 0x4E;        // quad_perm [2, 3, 0, 1]
+constexpr int kHalfMirror = 0x141;  // row_half_mirror: the other quad of eight lanes
+
 template <int CTRL>
-__device__ __forceinline__ double dpp_f64(double v) {
+__device__ __forceinline__ float dpp(float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(v)), CTRL, 0xF, 0xF, false));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
     const uint64_t u = __builtin_bit_cast(uint64_t, v);
     const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(u), CTRL, 0xF, 0xF, false);
     const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(u >> 32), CTRL, 0xF, 0xF, false);
     return __builtin_bit_cast(double, (static_cast<uint64_t>(hi) << 32) | lo);
 }
-constexpr int kSwap1 = 0xB1;        // quad_perm [1, 0, 3, 2]
-constexpr int kSwap2 = 0x4E;        // quad_perm [2, 3, 0, 1]
-constexpr int kHalfMirror = 0x141;  // row_half_mirror: the other quad of eight lanes
+// The largest of a block's lanes (4 or 8 neighbours).
+template <int BLANES, typename F>
+__device__ __forceinline__ F block_max(F v) {
+    F o = dpp<kSwap1>(v);
+    v = o > v ? o : v;
+    o = dpp<kSwap2>(v);
+    v = o > v ? o : v;
+    if constexpr (BLANES == 8) {
+        o = dpp<kHalfMirror>(v);
+        v = o > v ? o : v;
+    }
+    return v;
+}
+// max(|a|, |b|, c), a NaN being nothing
+__device__ __forceinline__ float max_abs(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, |%1|, |%2|, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 
+// 1 / n to within 2^-51: two Newton steps on the instruction's estimate.
+__device__ __forceinline__ double inverse(double n) {
+    double r = __builtin_amdgcn_rcp(n);
+    r = __builtin_fma(__builtin_fma(-n, r, 1.0), r, r);
+    return __builtin_fma(__builtin_fma(-n, r, 1.0), r, r);
+}
+
+// acc += the lane's channels of rows b .. e of a plane; O holds the plane's byte offsets.
+template <int DT, int D, typename O>
+__device__ __forceinline__ void add_rows(const typename vz::Elem<DT>::T* __restrict__ src, int32_t b, int32_t e,
+                                         int lane, double (&acc)[vz::Elem<DT>::kPer16B]) {
+    constexpr int PER = vz::Elem<DT>::kPer16B;
+    constexpr uint32_t STEP = D * sizeof(typename vz::Elem<DT>::T);
+    constexpr int ROWS = 8;
+    if (b >= e) return;
+    const char* const base = reinterpret_cast<const char*>(src);
+    O at = static_cast<O>(b) * STEP + lane * 16;
+    const O last = static_cast<O>(e - 1) * STEP + lane * 16;
+    // eight rows' loads at a time, those past the span reading its last row again and adding nothing
+    for (int32_t left = e - b; left > 0; left -= ROWS, at += ROWS * STEP) {
+        uint4 x[ROWS];
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const O o = at + u * STEP;
+            // (32 bits: the offset may wrap in the plane's last rows)
+            x[u] = *reinterpret_cast<const uint4*>(base + (u < left ? o : last));
+        }
+        // (all loads are on their way before the first branch: the compiler would move each behind its own)
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            if (u < left) {
+                float f[PER];
+                vz::unpack16<DT>(x[u], f);
+#pragma unroll
+                for (int i = 0; i < PER; ++i) acc[i] += f[i];
+            }
+        }
+    }
+}
+
+// Codes of sums that are float32 numbers, which those of bfloat16 rows nearly
+// always are, come from the conversion instruction (nearest, ties to even, the
+// scale's exponent taken off first), applied to x / n rounded to 64 bits and
+// then to 32.  That is code_of's answer: x = M g and a border times n, B = m h,
+// are multiples of powers of two g and h, where M < 2^24 and x <= 28 n h, so
+// they are equal or differ by the smaller of g and h at least, which is more
+// than (1 + 2^-24) 2^-24 x for n below 2^19; x / n then is on the border, or more
+// than half a float32 step and 2^-48 of it away, and stays on its side.  (Not
+// where x / n may lie below the normal floats.)
+constexpr double kMostExact = 1 << 19;
 template <int DT, int D, bool RAG>
 __global__ __launch_bounds__(256) void fuse_q4_kernel(const FuseArgs a, const VzQ4Cache out) {
     using E = vz::Elem<DT>;
@@ -43,7 +119,6 @@ __global__ __launch_bounds__(256) void fuse_q4_kernel(const FuseArgs a, const Vz
     constexpr int LANES = D / PER;               // lanes per span row
     constexpr int SPB = 256 / LANES;             // spans per block
     constexpr int BLANES = vz_q4::kBlock / PER;  // lanes per block of channels
-    constexpr int ROWS = 4;                      // rows in flight per lane
 
     const int sub = threadIdx.x / LANES;
     const int lane = threadIdx.x % LANES;
@@ -72,25 +147,15 @@ __global__ __launch_bounds__(256) void fuse_q4_kernel(const FuseArgs a, const Vz
     b = b < 0 ? 0 : (b > T_in ? T_in : b);
     e = e < b ? b : (e > T_in ? T_in : e);
 
-    const T* src = static_cast<const T*>(which ? a.v_in : a.k_in) +
-                   ((static_cast<size_t>(l) * a.H + h) * static_cast<size_t>(a.in_plane) + in_row) * D + lane * PER;
+    const T* const src = static_cast<const T*>(which ? a.v_in : a.k_in) +
+                         ((static_cast<size_t>(l) * a.H + h) * static_cast<size_t>(a.in_plane) + in_row) * D;
     double acc[PER];
 #pragma unroll
     for (int i = 0; i < PER; ++i) acc[i] = 0.0;
-    // four rows' loads at a time, those past the span reading its last row again and adding nothing
-    for (int32_t r = b; r < e; r += ROWS) {
-        uint4 x[ROWS];
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u)
-            x[u] = *reinterpret_cast<const uint4*>(src + static_cast<size_t>(min(r + u, e - 1)) * D);
-#pragma unroll
-        for (int u = 0; u < ROWS; ++u) {
-            float f[PER];
-            vz::unpack16<DT>(x[u], f);
-#pragma unroll
-            for (int i = 0; i < PER; ++i) acc[i] += r + u < e ? f[i] : 0.f;
-        }
-    }
+    if (T_in <= (INT64_C(1) << 32) / (D * static_cast<int>(sizeof(T))))
+        add_rows<DT, D, uint32_t>(src, b, e, lane, acc);
+    else
+        add_rows<DT, D, uint64_t>(src, b, e, lane, acc);
     const double n = max(e - b, 1);
     const T* anchor = static_cast<const T*>(which ? a.av : a.ak);
     const size_t orow = (static_cast<size_t>(l) * a.H + h) * static_cast<size_t>(a.out_plane) + out_row + j;
@@ -103,22 +168,42 @@ __global__ __launch_bounds__(256) void fuse_q4_kernel(const FuseArgs a, const Vz
 #pragma unroll
         for (int i = 0; i < PER; ++i) acc[i] = __builtin_fma(n, f[i], acc[i]);
     }
-    double top = 0.0;
-    bool bad = false;
+    float sum[PER];
+    bool exact = true;  // every sum of this lane is a float32
+    float top = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const double x = __builtin_fabs(acc[i]);
-        bad = bad || !(x < INFINITY);
-        top = __builtin_fmax(top, x);
+        sum[i] = static_cast<float>(acc[i]);
+        exact = exact && static_cast<double>(sum[i]) == acc[i];
     }
-    top = bad ? INFINITY : top;
-    top = __builtin_fmax(top, dpp_f64<kSwap1>(top));
-    top = __builtin_fmax(top, dpp_f64<kSwap2>(top));
-    if constexpr (BLANES == 8) top = __builtin_fmax(top, dpp_f64<kHalfMirror>(top));
-    const vz_q4::Scale s = vz_q4::scale_for(top, n);
-    uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) w |= vz_q4::code_of(acc[i], s.unit) << (4 * i);
+    for (int i = 0; i < PER; i += 2) top = max_abs(sum[i], sum[i + 1], top);
+    vz_q4::Scale s = vz_q4::scale_for(block_max<BLANES>(top), n);
+    uint32_t w = 0;
+    if (__all(exact && s.byte != vz_q4::kNoScale && (s.byte > vz_q4::kMinExp + 127 || top == 0.f) && n < kMostExact)) {
+        const double inv = inverse(n);
+        const float scale = __uint_as_float(static_cast<uint32_t>(s.byte) << 23);
+        float y[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) y[i] = static_cast<float>(acc[i] * inv);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[0], y[1], scale, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
+        if constexpr (PER == 8) {
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
+            w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
+        }
+    } else {
+        double most = 0.0;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            most = __builtin_fmax(most, __builtin_fabs(acc[i]));
+            fine = fine && __builtin_fabs(acc[i]) < INFINITY;  // (a NaN is lost in the maximum)
+        }
+        s = vz_q4::scale_for(block_max<BLANES>(fine ? most : INFINITY), n);
+#pragma unroll
+        for (int i = 0; i < PER; ++i) w |= vz_q4::code_of(acc[i], s.unit) << (4 * i);
+    }
     uint8_t* const codes = (which ? out.vc : out.kc) + orow * R::kCodes;
     if constexpr (PER == 8) {
         *reinterpret_cast<uint32_t*>(codes + 4 * lane) = w;

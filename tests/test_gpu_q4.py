@@ -149,6 +149,23 @@ def test_fused_rows_bit_for_bit(dtype, d, L, H, T, anchor):
     assert not from_dev(s)[:, :n].any() and (from_dev(s)[:, n:] == 9).all()
 
 
+def test_a_plane_of_more_than_4_gib_is_fused():
+    T, d, step = (1 << 24) + 77, 128, 64
+    x = torch().empty(1, 1, T, d, dtype=torch().bfloat16, device="cuda").fill_(1.0)
+    rng = np.random.default_rng(5)
+    tail = store(hard_rows(rng, 4096, d), BF16)
+    x[0, 0, T - 4096:] = to_dev(tail)
+    off = np.concatenate([np.arange(0, T - 4096, step), np.arange(T - 4096, T, 3), [T]]).astype(np.int32)
+    n, m = len(off) - 1, len(np.arange(T - 4096, T, 3))
+    cache = vz().q4_cache(1, 1, n, d)
+    s, p = torch().empty(1, n, device="cuda"), torch().empty(1, n, dtype=torch().int32, device="cuda")
+    vz().voxzip_fuse_spans_q4(x, x, to_dev(off), *cache, s, p)
+    codes, scales = q4ref.span_means(widen(tail, BF16)[None, None], off[n - m:] - off[n - m])
+    for got, want in zip(cache, (codes, scales) * 2):
+        assert np.array_equal(from_dev(got[:, :, n - m:]), want)
+        assert (got[:, :, :n - m] == (0x66 if got.shape[-1] == d // 2 else 127 - 2)).all()  # 1 = 4 * 2^-2
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_blocks_that_are_not_finite_read_as_nan(dtype):
     x = np.ones((1, 1, 4, 128), dtype=np.float32)
