@@ -1,7 +1,7 @@
 """A decode loop over a batch of sequences, on the ragged entry points.
 
-The cache of every sequence lives in one packed ``[L][Hkv][total][d]`` cache
-(sequence s at slots ``seq_base[s] ..``), and the per-sequence lengths,
+The cache of every sequence lives in one packed ``[L][Hkv][total][d]`` cache,
+at its own precision or 4-bit (sequence s at slots ``seq_base[s] ..``), and the per-sequence lengths,
 positions and budgets live in device arrays.  No step of the loop reads a
 length back to the host, so a whole decode step can be captured once in a HIP
 graph and replayed for every token:
@@ -33,8 +33,9 @@ from __future__ import annotations
 
 import numpy as np
 
-from . import (VZ_OP_DECODE, VZ_OP_EVICT, voxzip_decode_attend_score_ragged, voxzip_evict_compact_ragged,
-               voxzip_fuse_spans_ragged, workspace_ragged)
+from . import (VZ_OP_DECODE, VZ_OP_DECODE_Q4, VZ_OP_EVICT, q4_cache, voxzip_decode_attend_score_q4_ragged,
+               voxzip_decode_attend_score_ragged, voxzip_evict_compact_q4_ragged, voxzip_evict_compact_ragged,
+               voxzip_fuse_spans_q4_ragged, voxzip_fuse_spans_ragged, workspace_ragged)
 
 
 class DecodeLoop:
@@ -45,13 +46,20 @@ class DecodeLoop:
     caller fills the cache with :meth:`fuse` (or writes ``k``, ``v``,
     ``score``, ``pos`` and :meth:`set_lengths` itself), or retires slots and
     admits requests into them one by one (:meth:`retire`, :meth:`admit`).
+
+    ``bits=4`` keeps the cache as 4-bit rows (``planes``: k_codes, k_scales,
+    v_codes, v_scales, see :func:`q4_cache`) instead of ``k`` and ``v``
+    (``planes``: k, v), in 3.76 times fewer bytes than bfloat16; prefills,
+    new rows, queries and outputs stay in ``dtype``.
     """
 
     NEVER = 1 << 30  # budget of a sequence whose eviction is not due this step
 
     def __init__(self, n_layers, n_q_heads, kv_heads, d, caps, budgets, gamma, interval=1, n_sink=4,
-                 n_recent=-1, dtype=None, device="cuda"):
+                 n_recent=-1, dtype=None, device="cuda", bits=None):
         import torch
+        if bits not in (None, 4):
+            raise ValueError(f"bits must be None (rows of dtype) or 4, not {bits}")
         self.torch = torch
         dtype = torch.bfloat16 if dtype is None else dtype
         self.L, self.Hq, self.Hkv, self.d = n_layers, n_q_heads, kv_heads, d
@@ -77,15 +85,24 @@ class DecodeLoop:
         self._never = torch.full((self.n,), self.NEVER, dtype=torch.int32, device=device)
         self._eff_budget = torch.zeros_like(self.length)
         L, H = n_layers, kv_heads
-        self.k = torch.zeros(L, H, self.total, d, dtype=dtype, device=device)
-        self.v = torch.zeros_like(self.k)
+        if bits == 4:
+            self.planes = q4_cache(L, H, self.total, d, device)
+            self._fuse_call, self._decode_call, self._evict_call = (
+                voxzip_fuse_spans_q4_ragged, voxzip_decode_attend_score_q4_ragged, voxzip_evict_compact_q4_ragged)
+        else:
+            self.k = torch.zeros(L, H, self.total, d, dtype=dtype, device=device)
+            self.v = torch.zeros_like(self.k)
+            self.planes = (self.k, self.v)
+            self._fuse_call, self._decode_call, self._evict_call = (
+                voxzip_fuse_spans_ragged, voxzip_decode_attend_score_ragged, voxzip_evict_compact_ragged)
         self.score = torch.zeros(L, self.total, dtype=torch.float32, device=device)
         self.pos = torch.zeros(L, self.total, dtype=torch.int32, device=device)
         self.out = torch.zeros(self.n, L, n_q_heads, d, dtype=dtype, device=device)
         self.out_layers = [torch.zeros(self.n, 1, n_q_heads, d, dtype=dtype, device=device) for _ in range(L)]
         # per-layer calls use one-layer views of the same planes
-        self.ws_all = workspace_ragged(VZ_OP_DECODE, L, n_q_heads, kv_heads, d, self.total, self.n, device)
-        self.ws_layer = workspace_ragged(VZ_OP_DECODE, 1, n_q_heads, kv_heads, d, self.total, self.n, device)
+        op = VZ_OP_DECODE_Q4 if bits == 4 else VZ_OP_DECODE
+        self.ws_all = workspace_ragged(op, L, n_q_heads, kv_heads, d, self.total, self.n, device)
+        self.ws_layer = workspace_ragged(op, 1, n_q_heads, kv_heads, d, self.total, self.n, device)
         self.ws_evict = workspace_ragged(VZ_OP_EVICT, L, n_q_heads, kv_heads, d, self.total, self.n, device)
         self.steps = 0
         self._graphs = {}
@@ -99,8 +116,8 @@ class DecodeLoop:
     def fuse(self, k_in, v_in, in_base, T_in, span_off, off_base, n_spans, max_spans):
         """Stage-1 fusion of every sequence's prefill into the packed cache;
         lengths and positions start at the span counts."""
-        voxzip_fuse_spans_ragged(k_in, v_in, in_base, T_in, span_off, off_base, n_spans, max_spans, self.k,
-                                 self.v, self.score, self.pos, self.seq_base, self.cap, status=self.status)
+        self._fuse_call(k_in, v_in, in_base, T_in, span_off, off_base, n_spans, max_spans, *self.planes, self.score,
+                        self.pos, self.seq_base, self.cap, status=self.status)
         self.length.copy_(n_spans)
         self.next_pos.copy_(n_spans)
         self.age.zero_()
@@ -131,14 +148,13 @@ class DecodeLoop:
         n_spans = int(span_off.numel()) - 1
         if n_spans < 1 or n_spans + 1 > self.slot_cap[s]:
             raise ValueError(f"{n_spans} spans do not fit slot {s} of {self.slot_cap[s]} slots with a free one")
-        dev = lambda a, dt: torch.tensor(a, dtype=dt, device=self.k.device)
+        dev = lambda a, dt: torch.tensor(a, dtype=dt, device=self.score.device)
         one = np.zeros(self.n, dtype=np.int64)
         at = lambda x: np.where(np.arange(self.n) == s, x, 0)
         cap_adm = at(self.slot_cap[s])  # every other slot idle for this call
-        voxzip_fuse_spans_ragged(k_in, v_in, dev(one, torch.int64), dev(at(T_in), torch.int32), span_off,
-                                 dev(one, torch.int64), dev(at(n_spans), torch.int32), n_spans, self.k, self.v,
-                                 self.score, self.pos, self.seq_base, dev(cap_adm, torch.int32),
-                                 status=self.status)
+        self._fuse_call(k_in, v_in, dev(one, torch.int64), dev(at(T_in), torch.int32), span_off,
+                        dev(one, torch.int64), dev(at(n_spans), torch.int32), n_spans, *self.planes, self.score,
+                        self.pos, self.seq_base, dev(cap_adm, torch.int32), status=self.status)
         self.length[s] = n_spans
         self.next_pos[s] = n_spans
         self.age[s] = 0
@@ -151,17 +167,15 @@ class DecodeLoop:
 
     # ---- one step ----
     def _decode_all(self, q, k_new, v_new):
-        voxzip_decode_attend_score_ragged(q, k_new, v_new, self.k, self.v, self.score, self.pos, self.out,
-                                          self.seq_base, self.cap, self.length, self.next_pos, self.gamma,
-                                          status=self.status, workspace=self.ws_all)
+        self._decode_call(q, k_new, v_new, *self.planes, self.score, self.pos, self.out, self.seq_base, self.cap,
+                          self.length, self.next_pos, self.gamma, status=self.status, workspace=self.ws_all)
 
     def _decode_layers(self, q, k_new, v_new, layer_query):
         for l in range(self.L):
             ql = layer_query(l, q, self.out_layers)  # [n][1][Hq][d]; may read out_layers[l - 1]
-            voxzip_decode_attend_score_ragged(
-                ql, k_new[l], v_new[l], self.k[l: l + 1], self.v[l: l + 1], self.score[l: l + 1],
-                self.pos[l: l + 1], self.out_layers[l], self.seq_base, self.cap, self.length, self.next_pos,
-                self.gamma, status=self.status, workspace=self.ws_layer)
+            self._decode_call(ql, k_new[l], v_new[l], *(x[l: l + 1] for x in self.planes), self.score[l: l + 1],
+                              self.pos[l: l + 1], self.out_layers[l], self.seq_base, self.cap, self.length,
+                              self.next_pos, self.gamma, status=self.status, workspace=self.ws_layer)
 
     def _evict(self):
         budget = self.budget
@@ -172,9 +186,9 @@ class DecodeLoop:
             torch.eq(self._rem, 0, out=self._due)
             torch.where(self._due, self.budget, self._never, out=self._eff_budget)
             budget = self._eff_budget
-        voxzip_evict_compact_ragged(self.k, self.v, self.score, self.pos, self.seq_base, self.cap, self.length,
-                                    budget, self.next_pos, n_sink=self.n_sink, n_recent=self.n_recent,
-                                    new_len_out=self.new_len, status=self.status, workspace=self.ws_evict)
+        self._evict_call(*self.planes, self.score, self.pos, self.seq_base, self.cap, self.length, budget,
+                         self.next_pos, n_sink=self.n_sink, n_recent=self.n_recent, new_len_out=self.new_len,
+                         status=self.status, workspace=self.ws_evict)
         self.length.copy_(self.new_len)
 
     def _step(self, q, k_new, v_new, layer_query, evict):
@@ -211,7 +225,7 @@ class DecodeLoop:
         One eager warm-up step runs first; the state is restored afterwards,
         so capture() leaves the cache as it found it."""
         torch = self.torch
-        state = (self.k, self.v, self.score, self.pos, self.length, self.next_pos, self.age)
+        state = (*self.planes, self.score, self.pos, self.length, self.next_pos, self.age)
         saved = [t.clone() for t in state]
         stream = torch.cuda.Stream()
         stream.wait_stream(torch.cuda.current_stream())
