@@ -392,8 +392,10 @@ def q4_cache(n_layers: int, kv_heads: int, cap: int, d: int, device="cuda"):
     return plane(d // 2), plane(d // 32), plane(d // 2), plane(d // 32)
 
 
-def _expect_q4(d, k_codes, k_scales, v_codes, v_scales):
-    """Checks a 4-bit cache of head size d and returns (L, H, slots)."""
+def _expect_q4(d, k_codes, k_scales, v_codes, v_scales, *others):
+    """Checks a 4-bit cache of head size d, and that it and the call's other
+    tensors are on the current device (whose stream the kernels are launched
+    on); returns (L, H, slots)."""
     import torch
     if d not in (64, 128):
         raise ValueError(f"head size must be 64 or 128, not {d}")
@@ -403,6 +405,12 @@ def _expect_q4(d, k_codes, k_scales, v_codes, v_scales):
     u8, codes, scales = torch.uint8, (L, H, cap, d // 2), (L, H, cap, d // 32)
     _expect_all(((k_codes, codes, "k_codes", u8), (k_scales, scales, "k_scales", u8), (v_codes, codes, "v_codes", u8),
                  (v_scales, scales, "v_scales", u8)))
+    device = k_codes.get_device()
+    for t in (k_scales, v_codes, v_scales, *others):
+        if t is not None and t.get_device() != device:
+            raise ValueError("tensors must be on one device")
+    if device >= 0 and device != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device")
     return L, H, cap
 
 
@@ -412,7 +420,8 @@ def voxzip_fuse_spans_q4(k_in, v_in, span_off, k_codes, k_scales, v_codes, v_sca
     int32 [n+1] on the device.  Spans of length 1 pack rows as they are."""
     import torch
     L, H, T_in, d = k_in.shape
-    cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)[2]
+    cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, k_in, v_in, span_off,
+                     score_out, pos_out, anchor_k, anchor_v)[2]
     n = span_off.numel() - 1
     dt, span_shape = k_in.dtype, (L, H, n, d)
     _expect_all(((k_codes, (L, H, cap, d // 2), "k_codes", None), (v_in, (L, H, T_in, d), "v_in", dt),
@@ -431,6 +440,10 @@ def voxzip_unpack_q4(codes, scales, out, stream=None) -> None:
     import torch
     d = out.shape[-1]
     rows = tuple(out.shape[:-1])
+    if not codes.get_device() == scales.get_device() == out.get_device():
+        raise ValueError("tensors must be on one device")
+    if out.is_cuda and out.get_device() != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device")
     _expect_all(((codes, rows + (d // 2,), "codes", torch.uint8), (scales, rows + (d // 32,), "scales", torch.uint8)))
     n = out.numel() // d if d else 0
     if n == 0:
@@ -443,7 +456,8 @@ def voxzip_decode_attend_score_q4(q, k_new, v_new, k_codes, k_scales, v_codes, v
     """One decode step over all layers of a 4-bit cache; q/out [L][Hq][d]."""
     import torch
     Hq, d = q.shape[1:]
-    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, q, k_new, v_new, score, pos,
+                             out, workspace)
     dt = q.dtype
     rows, new_rows, plane = (L, Hq, d), (L, Hkv, d), (L, cap)
     _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
@@ -461,7 +475,8 @@ def voxzip_evict_compact_q4(k_codes, k_scales, v_codes, v_scales, score, pos, le
     """Stage-2 eviction of a 4-bit cache, in place; returns the new resident length."""
     import torch
     d = 2 * k_codes.shape[-1]
-    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, score, pos, kept_pos_out,
+                             workspace)
     _expect_all(((score, (L, cap), "score", torch.float32), (pos, (L, cap), "pos", torch.int32),
                  (kept_pos_out, (L, int(budget)), "kept_pos_out", torch.int32)))
     new_len = ctypes.c_int32(0)
@@ -480,7 +495,8 @@ def voxzip_decode_evict_q4(q, k_new, v_new, k_codes, k_scales, v_codes, v_scales
     new resident length."""
     import torch
     Hq, d = q.shape[1:]
-    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, q, k_new, v_new, score, pos,
+                             out, kept_pos_out, workspace)
     dt = q.dtype
     rows, new_rows, plane = (L, Hq, d), (L, Hkv, d), (L, cap)
     _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
@@ -502,7 +518,8 @@ def voxzip_fuse_spans_q4_ragged(k_in, v_in, in_base, T_in, span_off, off_base, n
     cache; k_in/v_in [L][H][total_in][d], anchors [L][H][total][d]."""
     import torch
     L, H, total_in, d = k_in.shape
-    total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)[2]
+    total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, k_in, v_in, in_base, T_in,
+                       span_off, off_base, n_spans, score_out, pos_out, seq_base, cap, status, anchor_k, anchor_v)[2]
     n = seq_base.numel()
     dt, out_shape = k_in.dtype, (L, H, total, d)
     if span_off.dtype != torch.int32 or span_off.dim() != 1:
@@ -527,7 +544,8 @@ def voxzip_decode_attend_score_q4_ragged(q, k_new, v_new, k_codes, k_scales, v_c
     cache; q/out [S][L][Hq][d], k_new/v_new [S][L][Hkv][d]."""
     import torch
     n, _, Hq, d = q.shape
-    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, q, k_new, v_new, score,
+                               pos, out, seq_base, cap, length, next_pos, status, workspace)
     dt = q.dtype
     rows, new_rows, plane = (n, L, Hq, d), (n, L, Hkv, d), (L, total)
     _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
@@ -549,7 +567,8 @@ def voxzip_evict_compact_q4_ragged(k_codes, k_scales, v_codes, v_scales, score, 
     cache; new_len_out (int32 [S], device) receives min(length, budget)."""
     import torch
     d = 2 * k_codes.shape[-1]
-    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
+    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, score, pos, seq_base, cap,
+                               length, budget, next_pos, kept_pos_out, new_len_out, status, workspace)
     n, plane = seq_base.numel(), (L, total)
     _expect_all(((score, plane, "score", torch.float32), (pos, plane, "pos", torch.int32),
                  (kept_pos_out, plane, "kept_pos_out", torch.int32)))

@@ -528,6 +528,38 @@ def test_a_captured_step_replays():
                 assert t.equal(x, y), (r, i)
 
 
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """Told on the host, with a card's number that is not the tensors'."""
+    m, t, n = vz(), torch(), 1
+    c = Case(1, 1, 2, 1, 64, 4, BF16)
+    cache, s, p = c.dev()
+    q, kn, _ = (to_dev(x) for x in c.rows())
+    out, ln, base = t.zeros_like(q), i32([n]), i64([0])
+    rows, off = t.zeros(1, 1, 4, 64, dtype=t.bfloat16, device="cuda"), i32([0, 2, 4])
+    calls = [
+        lambda: m.voxzip_fuse_spans_q4(rows, rows, off, *cache, s, p),
+        lambda: m.voxzip_unpack_q4(cache[0], cache[1], rows),
+        lambda: m.voxzip_decode_attend_score_q4(q, kn, kn, *cache, s, p, out, n, n, 0.9),
+        lambda: m.voxzip_evict_compact_q4(*cache, s, p, 3, 2, 3),
+        lambda: m.voxzip_decode_evict_q4(q, kn, kn, *cache, s, p, out, n, n, 0.9, 2),
+        lambda: m.voxzip_fuse_spans_q4_ragged(rows, rows, base, ln, off, base, ln, 2, *cache, s, p, base, ln),
+        lambda: m.voxzip_decode_attend_score_q4_ragged(q[None], kn[None], kn[None], *cache, s, p, out[None], base, ln,
+                                                       ln, ln, 0.9),
+        lambda: m.voxzip_evict_compact_q4_ragged(*cache, s, p, base, ln, ln, ln, ln)]
+    before = [x.clone() for x in (*cache, s, p, out, rows)]
+    monkeypatch.setattr(t.cuda, "current_device", lambda: 1)
+    for call in calls:
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    s, full = s.cpu(), s
+    for call in calls[:1] + calls[2:]:
+        with pytest.raises(ValueError, match="one device"):
+            call()
+    monkeypatch.undo()
+    for x, y in zip((*cache, full, p, out, rows), before):
+        assert t.equal(x, y)
+
+
 def test_slots_beyond_four_gigabytes():
     """Codes whose byte offsets pass 2^32 in one plane set."""
     m, t, L, Hq, Hkv, d, cap, length = vz(), torch(), 3, 2, 2, 128, 12_000_000, 200
