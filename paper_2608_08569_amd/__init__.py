@@ -392,10 +392,8 @@ def q4_cache(n_layers: int, kv_heads: int, cap: int, d: int, device="cuda"):
     return plane(d // 2), plane(d // 32), plane(d // 2), plane(d // 32)
 
 
-def _expect_q4(d, k_codes, k_scales, v_codes, v_scales, *others):
-    """Checks a 4-bit cache of head size d, and that it and the call's other
-    tensors are on the current device (whose stream the kernels are launched
-    on); returns (L, H, slots)."""
+def _expect_q4(d, k_codes, k_scales, v_codes, v_scales):
+    """Checks a 4-bit cache of head size d and returns (L, H, slots)."""
     import torch
     if d not in (64, 128):
         raise ValueError(f"head size must be 64 or 128, not {d}")
@@ -405,13 +403,28 @@ def _expect_q4(d, k_codes, k_scales, v_codes, v_scales, *others):
     u8, codes, scales = torch.uint8, (L, H, cap, d // 2), (L, H, cap, d // 32)
     _expect_all(((k_codes, codes, "k_codes", u8), (k_scales, scales, "k_scales", u8), (v_codes, codes, "v_codes", u8),
                  (v_scales, scales, "v_scales", u8)))
-    device = k_codes.get_device()
-    for t in (k_scales, v_codes, v_scales, *others):
-        if t is not None and t.get_device() != device:
-            raise ValueError("tensors must be on one device")
-    if device >= 0 and device != torch.cuda.current_device():
-        raise ValueError("tensors must be on the current device")
     return L, H, cap
+
+
+def _pointers(stream, *tensors):
+    """Stream handle and pointers of a call whose tensors have to be contiguous
+    and on the current device, whose stream the kernels are launched on."""
+    import torch
+    device, out = tensors[0].get_device(), []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        if t.get_device() != device:
+            raise ValueError("tensors must be on one device")
+        if not t.is_contiguous():
+            raise ValueError("tensors must be contiguous")
+        out.append(t.data_ptr())
+    if device < 0:
+        raise ValueError("tensors must be on the GPU")
+    if device != torch.cuda.current_device():
+        raise ValueError("tensors must be on the current device")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream, out
 
 
 def voxzip_fuse_spans_q4(k_in, v_in, span_off, k_codes, k_scales, v_codes, v_scales, score_out, pos_out,
@@ -420,18 +433,16 @@ def voxzip_fuse_spans_q4(k_in, v_in, span_off, k_codes, k_scales, v_codes, v_sca
     int32 [n+1] on the device.  Spans of length 1 pack rows as they are."""
     import torch
     L, H, T_in, d = k_in.shape
-    cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, k_in, v_in, span_off,
-                     score_out, pos_out, anchor_k, anchor_v)[2]
+    cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)[2]
     n = span_off.numel() - 1
     dt, span_shape = k_in.dtype, (L, H, n, d)
     _expect_all(((k_codes, (L, H, cap, d // 2), "k_codes", None), (v_in, (L, H, T_in, d), "v_in", dt),
                  (score_out, (L, cap), "score_out", torch.float32), (pos_out, (L, cap), "pos_out", torch.int32),
                  (span_off, (n + 1,), "span_off", torch.int32), (anchor_k, span_shape, "anchor_k", dt),
                  (anchor_v, span_shape, "anchor_v", dt)))
-    _check(lib().voxzip_fuse_spans_q4(_ptr(k_in), _ptr(v_in), T_in, _ptr(span_off), n, _ptr(anchor_k),
-                                      _ptr(anchor_v), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales),
-                                      _ptr(score_out), _ptr(pos_out), L, H, d, cap, _dtype_code(k_in),
-                                      _stream(stream)))
+    st, (k_p, v_p, off_p, *rest) = _pointers(stream, k_in, v_in, span_off, anchor_k, anchor_v, k_codes, k_scales, v_codes,
+                                             v_scales, score_out, pos_out)
+    _check(lib().voxzip_fuse_spans_q4(k_p, v_p, T_in, off_p, n, *rest, L, H, d, cap, _dtype_code(k_in), st))
 
 
 def voxzip_unpack_q4(codes, scales, out, stream=None) -> None:
@@ -440,15 +451,12 @@ def voxzip_unpack_q4(codes, scales, out, stream=None) -> None:
     import torch
     d = out.shape[-1]
     rows = tuple(out.shape[:-1])
-    if not codes.get_device() == scales.get_device() == out.get_device():
-        raise ValueError("tensors must be on one device")
-    if out.is_cuda and out.get_device() != torch.cuda.current_device():
-        raise ValueError("tensors must be on the current device")
     _expect_all(((codes, rows + (d // 2,), "codes", torch.uint8), (scales, rows + (d // 32,), "scales", torch.uint8)))
     n = out.numel() // d if d else 0
     if n == 0:
         return
-    _check(lib().voxzip_unpack_q4(_ptr(codes), _ptr(scales), n, d, _ptr(out), _dtype_code(out), _stream(stream)))
+    st, (c_p, s_p, out_p) = _pointers(stream, codes, scales, out)
+    _check(lib().voxzip_unpack_q4(c_p, s_p, n, d, out_p, _dtype_code(out), st))
 
 
 def voxzip_decode_attend_score_q4(q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out, length,
@@ -456,18 +464,15 @@ def voxzip_decode_attend_score_q4(q, k_new, v_new, k_codes, k_scales, v_codes, v
     """One decode step over all layers of a 4-bit cache; q/out [L][Hq][d]."""
     import torch
     Hq, d = q.shape[1:]
-    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, q, k_new, v_new, score, pos,
-                             out, workspace)
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
     dt = q.dtype
     rows, new_rows, plane = (L, Hq, d), (L, Hkv, d), (L, cap)
     _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
                  (v_new, new_rows, "v_new", dt), (score, plane, "score", torch.float32),
                  (pos, plane, "pos", torch.int32)))
-    _check(lib().voxzip_decode_attend_score_q4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_codes), _ptr(k_scales),
-                                               _ptr(v_codes), _ptr(v_scales), _ptr(score), _ptr(pos), _ptr(out),
-                                               int(length), int(next_pos), float(gamma), float(sm_scale), L, Hq, Hkv,
-                                               d, cap, _dtype_code(q), _ptr(workspace), _nbytes(workspace),
-                                               _stream(stream)))
+    st, (*state, ws) = _pointers(stream, q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out, workspace)
+    _check(lib().voxzip_decode_attend_score_q4(*state, int(length), int(next_pos), float(gamma), float(sm_scale), L, Hq,
+                                               Hkv, d, cap, _dtype_code(q), ws, _nbytes(workspace), st))
 
 
 def voxzip_evict_compact_q4(k_codes, k_scales, v_codes, v_scales, score, pos, length, budget, next_pos, n_sink=4,
@@ -475,15 +480,13 @@ def voxzip_evict_compact_q4(k_codes, k_scales, v_codes, v_scales, score, pos, le
     """Stage-2 eviction of a 4-bit cache, in place; returns the new resident length."""
     import torch
     d = 2 * k_codes.shape[-1]
-    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, score, pos, kept_pos_out,
-                             workspace)
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
     _expect_all(((score, (L, cap), "score", torch.float32), (pos, (L, cap), "pos", torch.int32),
                  (kept_pos_out, (L, int(budget)), "kept_pos_out", torch.int32)))
     new_len = ctypes.c_int32(0)
-    _check(lib().voxzip_evict_compact_q4(_ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score),
-                                         _ptr(pos), int(length), int(budget), int(n_sink), int(n_recent),
-                                         int(next_pos), _ptr(kept_pos_out), ctypes.byref(new_len), L, Hkv, d, cap,
-                                         _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    st, (*state, kept, ws) = _pointers(stream, k_codes, k_scales, v_codes, v_scales, score, pos, kept_pos_out, workspace)
+    _check(lib().voxzip_evict_compact_q4(*state, int(length), int(budget), int(n_sink), int(n_recent), int(next_pos),
+                                         kept, ctypes.byref(new_len), L, Hkv, d, cap, ws, _nbytes(workspace), st))
     return int(new_len.value)
 
 
@@ -495,19 +498,18 @@ def voxzip_decode_evict_q4(q, k_new, v_new, k_codes, k_scales, v_codes, v_scales
     new resident length."""
     import torch
     Hq, d = q.shape[1:]
-    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, q, k_new, v_new, score, pos,
-                             out, kept_pos_out, workspace)
+    L, Hkv, cap = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
     dt = q.dtype
     rows, new_rows, plane = (L, Hq, d), (L, Hkv, d), (L, cap)
     _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
                  (v_new, new_rows, "v_new", dt), (score, plane, "score", torch.float32),
                  (pos, plane, "pos", torch.int32), (kept_pos_out, (L, int(budget)), "kept_pos_out", torch.int32)))
     new_len = ctypes.c_int32(0)
-    _check(lib().voxzip_decode_evict_q4(_ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_codes), _ptr(k_scales),
-                                        _ptr(v_codes), _ptr(v_scales), _ptr(score), _ptr(pos), _ptr(out), int(length),
-                                        int(next_pos), float(gamma), float(sm_scale), int(budget), int(n_sink),
-                                        int(n_recent), _ptr(kept_pos_out), ctypes.byref(new_len), L, Hq, Hkv, d, cap,
-                                        _dtype_code(q), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    st, (*state, kept, ws) = _pointers(stream, q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out,
+                                       kept_pos_out, workspace)
+    _check(lib().voxzip_decode_evict_q4(*state, int(length), int(next_pos), float(gamma), float(sm_scale), int(budget),
+                                        int(n_sink), int(n_recent), kept, ctypes.byref(new_len), L, Hq, Hkv, d, cap,
+                                        _dtype_code(q), ws, _nbytes(workspace), st))
     return int(new_len.value)
 
 
@@ -518,8 +520,7 @@ def voxzip_fuse_spans_q4_ragged(k_in, v_in, in_base, T_in, span_off, off_base, n
     cache; k_in/v_in [L][H][total_in][d], anchors [L][H][total][d]."""
     import torch
     L, H, total_in, d = k_in.shape
-    total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, k_in, v_in, in_base, T_in,
-                       span_off, off_base, n_spans, score_out, pos_out, seq_base, cap, status, anchor_k, anchor_v)[2]
+    total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)[2]
     n = seq_base.numel()
     dt, out_shape = k_in.dtype, (L, H, total, d)
     if span_off.dtype != torch.int32 or span_off.dim() != 1:
@@ -527,14 +528,16 @@ def voxzip_fuse_spans_q4_ragged(k_in, v_in, in_base, T_in, span_off, off_base, n
     _expect_all(((k_codes, (L, H, total, d // 2), "k_codes", None), (v_in, (L, H, total_in, d), "v_in", dt),
                  (score_out, (L, total), "score_out", torch.float32), (pos_out, (L, total), "pos_out", torch.int32),
                  (anchor_k, out_shape, "anchor_k", dt), (anchor_v, out_shape, "anchor_v", dt)))
-    _check(lib().voxzip_fuse_spans_q4_ragged(
-        _ptr(k_in), _ptr(v_in), _seq_array(in_base, n, "int64", "in_base"), _seq_array(T_in, n, "int32", "T_in"),
-        total_in, _ptr(span_off), _seq_array(off_base, n, "int64", "off_base"),
-        _seq_array(n_spans, n, "int32", "n_spans"), span_off.numel(), int(max_spans), _ptr(anchor_k),
-        _ptr(anchor_v), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score_out), _ptr(pos_out),
-        _seq_array(seq_base, n, "int64", "seq_base"), _seq_array(cap, n, "int32", "cap"), total, n,
-        None if status is None else _seq_array(status, n, "int32", "status"), L, H, d, _dtype_code(k_in),
-        _stream(stream)))
+    i32, i64, one = torch.int32, torch.int64, (n,)
+    _expect_all(((in_base, one, "in_base", i64), (T_in, one, "T_in", i32), (off_base, one, "off_base", i64),
+                 (n_spans, one, "n_spans", i32), (seq_base, one, "seq_base", i64), (cap, one, "cap", i32),
+                 (status, one, "status", i32)))
+    st, (k_p, v_p, in_p, T_p, off_p, *rest, base_p, cap_p, status_p) = _pointers(
+        stream, k_in, v_in, in_base, T_in, span_off, off_base, n_spans, anchor_k, anchor_v, k_codes, k_scales, v_codes,
+        v_scales, score_out, pos_out, seq_base, cap, status)
+    _check(lib().voxzip_fuse_spans_q4_ragged(k_p, v_p, in_p, T_p, total_in, off_p, *rest[:2], span_off.numel(),
+                                             int(max_spans), *rest[2:], base_p, cap_p, total, n, status_p, L, H, d,
+                                             _dtype_code(k_in), st))
 
 
 def voxzip_decode_attend_score_q4_ragged(q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out,
@@ -544,20 +547,19 @@ def voxzip_decode_attend_score_q4_ragged(q, k_new, v_new, k_codes, k_scales, v_c
     cache; q/out [S][L][Hq][d], k_new/v_new [S][L][Hkv][d]."""
     import torch
     n, _, Hq, d = q.shape
-    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, q, k_new, v_new, score,
-                               pos, out, seq_base, cap, length, next_pos, status, workspace)
+    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
     dt = q.dtype
     rows, new_rows, plane = (n, L, Hq, d), (n, L, Hkv, d), (L, total)
     _expect_all(((q, rows, "q", dt), (out, rows, "out", dt), (k_new, new_rows, "k_new", dt),
                  (v_new, new_rows, "v_new", dt), (score, plane, "score", torch.float32),
                  (pos, plane, "pos", torch.int32)))
-    _check(lib().voxzip_decode_attend_score_q4_ragged(
-        _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score),
-        _ptr(pos), _ptr(out), _seq_array(seq_base, n, "int64", "seq_base"), _seq_array(cap, n, "int32", "cap"),
-        _seq_array(length, n, "int32", "length"), _seq_array(next_pos, n, "int32", "next_pos"), total, n,
-        float(gamma), float(sm_scale), L, Hq, Hkv, d, _dtype_code(q),
-        None if status is None else _seq_array(status, n, "int32", "status"), _ptr(workspace), _nbytes(workspace),
-        _stream(stream)))
+    i32, one = torch.int32, (n,)
+    _expect_all(((seq_base, one, "seq_base", torch.int64), (cap, one, "cap", i32), (length, one, "length", i32),
+                 (next_pos, one, "next_pos", i32), (status, one, "status", i32)))
+    st, (*state, status_p, ws) = _pointers(stream, q, k_new, v_new, k_codes, k_scales, v_codes, v_scales, score, pos, out,
+                                           seq_base, cap, length, next_pos, status, workspace)
+    _check(lib().voxzip_decode_attend_score_q4_ragged(*state, total, n, float(gamma), float(sm_scale), L, Hq, Hkv, d,
+                                                      _dtype_code(q), status_p, ws, _nbytes(workspace), st))
 
 
 def voxzip_evict_compact_q4_ragged(k_codes, k_scales, v_codes, v_scales, score, pos, seq_base, cap, length, budget,
@@ -567,16 +569,16 @@ def voxzip_evict_compact_q4_ragged(k_codes, k_scales, v_codes, v_scales, score, 
     cache; new_len_out (int32 [S], device) receives min(length, budget)."""
     import torch
     d = 2 * k_codes.shape[-1]
-    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales, score, pos, seq_base, cap,
-                               length, budget, next_pos, kept_pos_out, new_len_out, status, workspace)
+    L, Hkv, total = _expect_q4(d, k_codes, k_scales, v_codes, v_scales)
     n, plane = seq_base.numel(), (L, total)
     _expect_all(((score, plane, "score", torch.float32), (pos, plane, "pos", torch.int32),
                  (kept_pos_out, plane, "kept_pos_out", torch.int32)))
-    _check(lib().voxzip_evict_compact_q4_ragged(
-        _ptr(k_codes), _ptr(k_scales), _ptr(v_codes), _ptr(v_scales), _ptr(score), _ptr(pos),
-        _seq_array(seq_base, n, "int64", "seq_base"), _seq_array(cap, n, "int32", "cap"),
-        _seq_array(length, n, "int32", "length"), _seq_array(budget, n, "int32", "budget"),
-        _seq_array(next_pos, n, "int32", "next_pos"), total, n, int(n_sink), int(n_recent), _ptr(kept_pos_out),
-        None if new_len_out is None else _seq_array(new_len_out, n, "int32", "new_len_out"),
-        None if status is None else _seq_array(status, n, "int32", "status"), L, Hkv, d, _ptr(workspace),
-        _nbytes(workspace), _stream(stream)))
+    i32, one = torch.int32, (n,)
+    _expect_all(((seq_base, one, "seq_base", torch.int64), (cap, one, "cap", i32), (length, one, "length", i32),
+                 (budget, one, "budget", i32), (next_pos, one, "next_pos", i32), (new_len_out, one, "new_len_out", i32),
+                 (status, one, "status", i32)))
+    st, (*state, kept, new_len, status_p, ws) = _pointers(
+        stream, k_codes, k_scales, v_codes, v_scales, score, pos, seq_base, cap, length, budget, next_pos, kept_pos_out,
+        new_len_out, status, workspace)
+    _check(lib().voxzip_evict_compact_q4_ragged(*state, total, n, int(n_sink), int(n_recent), kept, new_len, status_p, L,
+                                                Hkv, d, ws, _nbytes(workspace), st))
