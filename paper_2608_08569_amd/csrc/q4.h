@@ -35,14 +35,6 @@ __device__ __forceinline__ uint32_t pair_bf16(uint32_t w, float scale) {
     __builtin_memcpy(&u, &r, 4);
     return u;
 }
-// Eight codes, one 32-bit word, as the eight bfloat16 of a matrix operand.
-__device__ __forceinline__ bf16x8_t eight_bf16(uint32_t w, float scale) {
-    const uint4 v = make_uint4(pair_bf16<0>(w, scale), pair_bf16<1>(w, scale), pair_bf16<2>(w, scale),
-                               pair_bf16<3>(w, scale));
-    bf16x8_t r;
-    __builtin_memcpy(&r, &v, 16);
-    return r;
-}
 // Byte b of a word of scales as a scale operand: one rotation that brings it to
 // the exponent field (rot = scale_rot(b)).
 __device__ __forceinline__ int scale_rot(int b) { return 9 + 8 * b; }

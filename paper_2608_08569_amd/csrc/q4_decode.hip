@@ -79,13 +79,14 @@ __global__ __launch_bounds__(kThreads, 4) void stats_kernel(const Q4Args a) {
         // the wave's units: 32 keys from c0 + 32 (share + shares i) on
         const int n_units = ((c1 - c0 + kUnit - 1) / kUnit - share + shares - 1) / shares;
         auto unit_key = [&](int i) { return c0 + kUnit * (share + shares * i); };
+        const int old = min(c1, it.len);  // end of the chunk's keys that the cache holds
         KTile kt[kStatsDepth];
         Queries<DT, D, PACK> q;
         q.load(static_cast<const typename vz::Elem<DT>::T*>(a.q) + row_g * G * D, lane, G);
         if (c == 0 && share == 0) q.store(parts_of_query<DT, D, PACK>(a, row_g));
         q.make();  // (the registers of the parts' making are the loads' then)
 #pragma unroll
-        for (int u = 0; u < kStatsDepth; ++u) load_k<D>(kt[u], lane, kc, ks, unit_key(u), it.len);
+        for (int u = 0; u < kStatsDepth; ++u) load_k<D>(kt[u], lane, kc, ks, unit_key(u), old);
         // the unit that holds the new key, when it is this wave's
         const int u_new = (it.len - c0) / kUnit;
         const bool mine = newest && u_new % shares == share;
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(kThreads, 4) void stats_kernel(const Q4Args a) {
             if (mine && k0 + kUnit > it.len) put_new_k<D>(k, lane, it.len - k0, s_new[w]);
             float x[PACK ? 1 : 2][4];
             dots_of<DT, D, PACK>(k, q, lane, k0, c1, x);
-            load_k<D>(k, lane, kc, ks, unit_key(i + kStatsDepth), it.len);  // (past the chunk: nothing)
+            load_k<D>(k, lane, kc, ks, unit_key(i + kStatsDepth), old);  // (past the chunk: nothing)
             m = fmaxf(m, fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])));
             if constexpr (!PACK) m = fmaxf(m, fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
             const float last = ref;

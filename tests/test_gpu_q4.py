@@ -447,6 +447,59 @@ def test_step_is_decode_then_evict(dtype, d, Hq, Hkv, L, length, budget, kept):
         assert t.equal(ka, kb)
 
 
+@pytest.mark.parametrize("budget,n_sink,n_recent", [
+    (1, 0, 0), (2, 0, 1), (5, 4, 0), (5, 4, 1), (40, 0, 0), (40, 39, 1), (40, 40, 0), (40, 0, 40)])
+@pytest.mark.parametrize("spread", [0, 1])
+def test_step_with_few_or_no_slots_that_compete(budget, n_sink, n_recent, spread):
+    """One slot over the budget, where sinks and recent positions protect most
+    of the slots or all, and where the scores are equal."""
+    m, t, L, Hq, Hkv, d = vz(), torch(), 2, 4, 2, 64
+    c = Case(budget, L, Hq, Hkv, d, budget + 1, BF16)
+    if not spread:
+        c.s[:] = 0
+    q, kn, vn = (to_dev(x) for x in c.rows())
+    if not spread:
+        q.zero_()  # every key weighs the same
+    results = []
+    for split in (True, False):
+        cache, s, p = c.dev()
+        out = t.zeros_like(q)
+        if split:
+            m.voxzip_decode_attend_score_q4(q, kn, vn, *cache, s, p, out, budget, budget + 2, 0.9,
+                                            workspace=m.workspace(m.VZ_OP_DECODE_Q4, L, Hq, Hkv, d, c.slots))
+            m.voxzip_evict_compact_q4(*cache, s, p, budget + 1, budget, budget + 3, n_sink, n_recent,
+                                      workspace=m.workspace(m.VZ_OP_EVICT, L, Hq, Hkv, d, c.slots))
+        else:
+            m.voxzip_decode_evict_q4(q, kn, vn, *cache, s, p, out, budget, budget + 2, 0.9, budget, n_sink, n_recent,
+                                     workspace=m.workspace(m.VZ_OP_DECODE_EVICT_Q4, L, Hq, Hkv, d, c.slots))
+        results.append([x[:, :, : budget] for x in cache] + [s[:, : budget], p[:, : budget], out])
+    for x, y in zip(*results):
+        assert t.equal(x, y)
+
+
+def test_calls_on_two_streams_at_once():
+    """Each call with a workspace of its own: the bits of the calls one after the other."""
+    m, t, L, Hq, Hkv, d = vz(), torch(), 8, 16, 2, 128
+    cases = [Case(i, L, Hq, Hkv, d, 2050, BF16) for i in range(2)]
+    rows = [[to_dev(x) for x in c.rows()] for c in cases]
+    streams = [t.cuda.Stream(), t.cuda.Stream()]
+    results = []
+    for together in (False, True):
+        state = [c.dev() for c in cases]
+        outs = [t.zeros_like(r[0]) for r in rows]
+        ws = [m.workspace(m.VZ_OP_DECODE_EVICT_Q4, L, Hq, Hkv, d, 2050) for _ in cases]
+        t.cuda.synchronize()
+        for step in range(4):
+            for i in range(2):
+                cache, s, p = state[i]
+                m.voxzip_decode_evict_q4(*rows[i], *cache, s, p, outs[i], 2049, 2055 + step, 0.9, 2049, workspace=ws[i],
+                                         stream=streams[i if together else 0])
+        t.cuda.synchronize()
+        results.append([x for (cache, s, p), o in zip(state, outs) for x in (*cache, s, p, o)])
+    for x, y in zip(*results):
+        assert t.equal(x, y)
+
+
 def test_a_request_from_prefill_to_eviction():
     """Fusion, decode steps past the budget and evictions in a row, each step
     checked against the oracle on the state before it; on a stream of its own."""
