@@ -404,7 +404,7 @@ VZ_API int voxzip_evict_compact_ragged(void *k_cache, void *v_cache, float *scor
  *  magnitude.  A block with an infinity or a NaN gets b = 255.
  *  Every value is exact in bfloat16 and float32.
  *  Codes must lie on 16-byte boundaries, scales on d / 32-byte ones
- *  (VZ_ERR_INVALID).
+ *  (VZ_ERR_INVALID); planes have at most 2^26 slots (VZ_ERR_SHAPE).
  */
 
 /*

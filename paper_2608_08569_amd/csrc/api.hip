@@ -145,8 +145,10 @@ VzQ4Cache q4_cache(void* kc, void* ks, void* vc, void* vs) {
 constexpr int64_t kUnpackMaxRows = int64_t(1) << 28;
 
 // The planes of a 4-bit cache: present, codes on 16-byte boundaries and scales
-// on a row's (the kernels' accesses).
-int check_q4(const char* fn, const VzQ4Cache& c, int32_t d) {
+// on a row's (the kernels' accesses), of a size whose slot numbers and grids
+// the kernels hold in 32 bits with room to spare.
+int check_q4(const char* fn, const VzQ4Cache& c, int32_t d, int64_t slots) {
+    if (slots > kRaggedMaxTotal) return fail(VZ_ERR_SHAPE, fn, "more than 2^26 slots");
     if (!c.kc || !c.ks || !c.vc || !c.vs) return fail(VZ_ERR_INVALID, fn, "null pointer");
     const uintptr_t codes = reinterpret_cast<uintptr_t>(c.kc) | reinterpret_cast<uintptr_t>(c.vc);
     const uintptr_t scales = reinterpret_cast<uintptr_t>(c.ks) | reinterpret_cast<uintptr_t>(c.vs);
@@ -547,7 +549,7 @@ int voxzip_fuse_spans_q4(const void* k_in, const void* v_in, int32_t T_in, const
     int rc = check_common(fn, n_layers, kv_heads, d, dtype);
     if (rc) return rc;
     const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
-    rc = check_q4(fn, c, d);
+    rc = check_q4(fn, c, d, cap_out);
     if (rc) return rc;
     if (2 * static_cast<int64_t>(kv_heads) > 65535) return fail(VZ_ERR_UNSUPPORTED, fn, "too many KV heads");
     if (T_in < 0 || n_spans < 0 || cap_out < 1) return fail(VZ_ERR_SHAPE, fn, "negative size");
@@ -589,7 +591,7 @@ int voxzip_decode_attend_score_q4(const void* q, const void* k_new, const void* 
                           n_layers, n_q_heads, kv_heads, d, cap, dtype);
     if (rc) return rc;
     const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
-    rc = check_q4(fn, c, d);
+    rc = check_q4(fn, c, d, cap);
     if (rc) return rc;
     const size_t need = vz_decode_q4_ws_bytes(n_layers, n_q_heads, kv_heads, d, cap, 0);
     if (!ws_ok(workspace, ws_bytes, need)) return fail(VZ_ERR_WORKSPACE, fn, "workspace missing, misaligned or too small");
@@ -609,7 +611,7 @@ int voxzip_evict_compact_q4(void* k_codes, void* k_scales, void* v_codes, void* 
     int rc = check_common(fn, n_layers, kv_heads, d, VZ_BF16);
     if (rc) return rc;
     const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
-    rc = check_q4(fn, c, d);
+    rc = check_q4(fn, c, d, cap);
     if (rc) return rc;
     int32_t M = 0;
     rc = check_evict(fn, len, budget, n_sink, n_recent, next_pos, kept_pos_out, cap, M);
@@ -639,7 +641,7 @@ int voxzip_decode_evict_q4(const void* q, const void* k_new, const void* v_new, 
                         need);
     if (rc) return rc;
     const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
-    rc = check_q4(fn, c, d);
+    rc = check_q4(fn, c, d, cap);
     if (rc) return rc;
     const size_t split = decode_evict_q4_split(n_layers, n_q_heads, kv_heads, d, cap);
     need = split + vz_evict_ws_bytes(n_layers, cap, 0);
@@ -684,7 +686,7 @@ int voxzip_fuse_spans_q4_ragged(const void* k_in, const void* v_in, const int64_
     int rc = check_ragged(fn, n_layers, kv_heads, d, dtype, total, n_seqs);
     if (rc) return rc;
     const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
-    rc = check_q4(fn, c, d);
+    rc = check_q4(fn, c, d, total);
     if (rc) return rc;
     if (total_in < 0 || total_off < 1 || max_spans < 0) return fail(VZ_ERR_SHAPE, fn, "negative size");
     if (total_in > kRaggedMaxTotal || max_spans > total) return fail(VZ_ERR_SHAPE, fn, "size out of range");
@@ -717,7 +719,7 @@ int voxzip_decode_attend_score_q4_ragged(const void* q, const void* k_new, const
     int rc = check_ragged(fn, n_layers, kv_heads, d, dtype, total, n_seqs);
     if (rc) return rc;
     const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
-    rc = check_q4(fn, c, d);
+    rc = check_q4(fn, c, d, total);
     if (rc) return rc;
     rc = check_heads(fn, n_q_heads, kv_heads);
     if (rc) return rc;
@@ -745,7 +747,7 @@ int voxzip_evict_compact_q4_ragged(void* k_codes, void* k_scales, void* v_codes,
     int rc = check_ragged(fn, n_layers, kv_heads, d, VZ_BF16, total, n_seqs);
     if (rc) return rc;
     const VzQ4Cache c = q4_cache(k_codes, k_scales, v_codes, v_scales);
-    rc = check_q4(fn, c, d);
+    rc = check_q4(fn, c, d, total);
     if (rc) return rc;
     if (n_sink < 0) return fail(VZ_ERR_INVALID, fn, "n_sink must be >= 0");
     if (new_len_out && overlaps(new_len_out, 4 * static_cast<size_t>(n_seqs), len, 4 * static_cast<size_t>(n_seqs)))

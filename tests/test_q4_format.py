@@ -153,6 +153,19 @@ def test_evict_q4_ragged_rejects(kw, code):
     assert vz.lib().voxzip_evict_compact_q4_ragged(*a.values(), None) == code
 
 
+def test_planes_of_more_than_2_26_slots_are_refused():
+    n, big, L = ctypes.c_int32(-7), (1 << 26) + 1, vz.lib()
+    ten, six = (FAKE,) * 10, (FAKE,) * 6
+    tail = (1, 4, 2, 128, big, vz.VZ_BF16, FAKE, 1 << 40, None)
+    assert L.voxzip_decode_attend_score_q4(*ten, 10, 10, 0.9, 0.0, *tail) == vz.VZ_ERR_SHAPE
+    assert L.voxzip_decode_evict_q4(*ten, 10, 10, 0.9, 0.0, 10, 4, -1, None, ctypes.byref(n), *tail) == vz.VZ_ERR_SHAPE
+    assert L.voxzip_evict_compact_q4(*six, 10, 5, 0, 0, 10, None, ctypes.byref(n), 1, 2, 128, big, FAKE, 1 << 40,
+                                     None) == vz.VZ_ERR_SHAPE
+    assert L.voxzip_fuse_spans_q4(FAKE, FAKE, 8, FAKE, 4, None, None, *six, 1, 2, 128, big, vz.VZ_BF16,
+                                  None) == vz.VZ_ERR_SHAPE
+    assert n.value == -7
+
+
 def test_workspace_sizes_grow_with_the_cache():
     size = vz.voxzip_workspace_bytes
     for op in (vz.VZ_OP_DECODE_Q4, vz.VZ_OP_DECODE_EVICT_Q4):
