@@ -13,7 +13,11 @@
 // rows are then exact but for extreme spreads, so a value's code does not turn
 // on the order of the rows, and a mean on a code's border is on it here as in
 // the definition.  gfx950 adds, compares and converts float64 at the float32
-// rate, and the call stays bound by its input.
+// rate; an element in is an unpacking, a conversion and an addition, one out
+// about ten instructions, so the kernel is near both its limits.  48 layers of
+// 32,768 rows (4 KV heads of 128, mean span 4): 719 us, 4.8 TB/s; with rows past
+// a span added as zeros and every code from comparisons: 946.  Unpacking runs at
+// 6.0 TB/s.
 #include <algorithm>
 
 #include "fuse_args.h"
@@ -85,7 +89,8 @@ __device__ __forceinline__ void add_rows(const typename vz::Elem<DT>::T* __restr
             // (32 bits: the offset may wrap in the plane's last rows)
             x[u] = *reinterpret_cast<const uint4*>(base + (u < left ? o : last));
         }
-        // (all loads are on their way before the first branch: the compiler would move each behind its own)
+        // (all loads are on their way before the first branch: the compiler would move each behind its own;
+        // one layer of 65,536 rows: 54 us so, 42 with four in flight, 36 with eight)
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
 #pragma unroll
