@@ -89,8 +89,8 @@ __device__ __forceinline__ void add_rows(const typename vz::Elem<DT>::T* __restr
             // (32 bits: the offset may wrap in the plane's last rows)
             x[u] = *reinterpret_cast<const uint4*>(base + (u < left ? o : last));
         }
-        // (all loads are on their way before the first branch: the compiler would move each behind its own;
-        // one layer of 65,536 rows: 54 us so, 42 with four in flight, 36 with eight)
+        // (all loads are on their way before the first branch, behind which the compiler would move each of its own:
+        // one layer of 65,536 rows takes 36 us, with four rows in flight 42, with the loads behind their branches 54)
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) asm volatile("" : "+v"(x[u].x), "+v"(x[u].y), "+v"(x[u].z), "+v"(x[u].w));
 #pragma unroll
