@@ -8,6 +8,7 @@
 #include <mutex>
 #include <string>
 
+#include "q4_calls.h"
 #include "vz_internal.h"
 
 // Scratch memory of voxzip_decode_evict_noalloc: one array per GPU, held

@@ -31,6 +31,7 @@
 #include <type_traits>
 
 #include "q4.h"
+#include "q4_calls.h"
 
 namespace vz_q4 {
 
@@ -161,7 +162,8 @@ __device__ __forceinline__ void load_k(KTile& k, int lane, const uint8_t* codes,
     const __amdgpu_buffer_rsrc_t rs = keys_of(scales, k0, n, kUnit, R::kScales);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const auto y = __builtin_amdgcn_raw_buffer_load_b128(rc, (16 * t + r16) * R::kCodes + 16 * block_of_lane<D>(lane), 0, 0);
+        const int off = (16 * t + r16) * R::kCodes + 16 * block_of_lane<D>(lane);
+        const auto y = __builtin_amdgcn_raw_buffer_load_b128(rc, off, 0, 0);
         __builtin_memcpy(k.w[t], &y, 16);
         if constexpr (D == 128) k.s[t] = __builtin_amdgcn_raw_buffer_load_b32(rs, (16 * t + r16) * 4, 0, 0);
         else k.s[t] = __builtin_amdgcn_raw_buffer_load_b16(rs, (16 * t + r16) * 2, 0, 0);
@@ -169,7 +171,8 @@ __device__ __forceinline__ void load_k(KTile& k, int lane, const uint8_t* codes,
 }
 
 template <int D>
-__device__ __forceinline__ void load_v(VTile<D>& v, int lane, const uint8_t* codes, const uint8_t* scales, int k0, int n) {
+__device__ __forceinline__ void load_v(VTile<D>& v, int lane, const uint8_t* codes, const uint8_t* scales, int k0,
+                                       int n) {
     using R = Rows<D>;
     const int q4 = lane >> 4, r16 = lane & 15;
     const __amdgpu_buffer_rsrc_t rc = keys_of(codes, k0, n, kUnit, R::kCodes);
@@ -293,6 +296,7 @@ struct Queries {
         }
     }
 };
+
 // Q . K of 32 keys (not yet scaled), -inf for keys at or past n (MASK).  PACK
 // (groups of at most 8 heads): set 0 holds head r16 & 7, keys 16 (r16 >> 3) +
 // 4 q4 + i, so that every exp2 serves a key and a head that exist; else set t
@@ -382,6 +386,7 @@ __device__ __forceinline__ void put_new_k(KTile& k, int lane, int key, const uin
             k.s[t] = s_new[Rows<D>::kCodes / 4];
         }
 }
+
 // acc[t] += P V of 32 keys: p of the lane's head (row of the result) and keys
 // 16 (e / 4) + 4 (lane / 16) + e % 4, in NP bfloat16 parts; lane: channels
 // D / 16 (lane % 16) + t of heads 4 (lane / 16) + i.

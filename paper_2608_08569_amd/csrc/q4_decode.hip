@@ -72,7 +72,8 @@ __global__ __launch_bounds__(kThreads, 4) void stats_kernel(const Q4Args a) {
     const int c0 = c * a.chunk, c1 = min(c0 + a.chunk, it.len + 1);  // the chunk's keys
     const size_t row_sl = static_cast<size_t>(it.s) * a.L + l;
     const bool newest = it.len < c1 && it.len >= c0;
-    if (newest && threadIdx.x == 0 && blockIdx.z == 0) a.pos[static_cast<size_t>(l) * a.plane + it.base + it.len] = it.next_pos;
+    if (newest && threadIdx.x == 0 && blockIdx.z == 0)
+        a.pos[static_cast<size_t>(l) * a.plane + it.base + it.len] = it.next_pos;
     const int item = blockIdx.z * kWaves + w;
     if (item < a.Hkv * shares) {
         const int g = item / shares, share = item - g * shares;
@@ -134,7 +135,8 @@ template <bool PACK>
 __device__ __forceinline__ float heads_sum(float v) {
     if constexpr (!PACK) return vz::row16_sum(v);
     auto dpp = [](float x, auto ctrl) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, false));
+        constexpr int CTRL = decltype(ctrl)::value;
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, false));
     };
     v += dpp(v, std::integral_constant<int, 0xB1>{});         // quad_perm [1, 0, 3, 2]
     v += dpp(v, std::integral_constant<int, 0x4E>{});         // quad_perm [2, 3, 0, 1]
@@ -297,7 +299,8 @@ __global__ __launch_bounds__(kThreads, DT == VZ_F32 && D == 128 && !PACK ? 2 : 3
     for (int i = 0; i < KEYS_PER_THREAD; ++i) {
         const int key = threadIdx.x + i * kThreads;
         if (c0 + key >= c1) continue;
-        const float now = fmaf(a.gamma, c0 + key < it.len ? a.score[slots + key] : 0.f, total[i]);  // (zero pad for the new slot)
+        // (zero pad for the new slot)
+        const float now = fmaf(a.gamma, c0 + key < it.len ? a.score[slots + key] : 0.f, total[i]);
         a.score[slots + key] = now;
         if (!RAG && a.ev_budget > 0) {
             const int32_t p = a.pos[slots + key];
@@ -408,13 +411,20 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(const Q4Args a) {
     dst[3] = vz::Elem<DT>::from_f32(o.w);
 }
 
-constexpr int kMostProducts = 6;  // float32, d = 128, groups of more than 8 heads
+// Room for a KV head's query parts: words of the larger, float32 form.
+constexpr int query_words(int d, bool pack) {
+    if (d == 64) return pack ? Queries<VZ_F32, 64, true>::kWords : Queries<VZ_F32, 64, false>::kWords;
+    return pack ? Queries<VZ_F32, 128, true>::kWords : Queries<VZ_F32, 128, false>::kWords;
+}
+// Groups of at most 8 heads take two parts of the queries a product.
+bool packs(int32_t Hq, int32_t Hkv) { return Hq / Hkv <= 8; }
 
 // Chunks per layer: kTargetChunks over the layers (two workgroups per CU: 8193
 // slots of 48 layers in 77 us, with three 81: each chunk costs its queries,
-// pairs and partial outputs, each missing one loads in flight), or what kMostKeys asks for
-// where that is more, and then as many as give every CU the same number of
-// workgroups (13,181 keys of 48 layers: 109 us in 13 chunks a layer, 103 in 16).
+// pairs and partial outputs, each missing one loads in flight), or what
+// kMostKeys asks for where that is more, and then as many as give every CU the
+// same number of workgroups (13,181 keys of 48 layers: 109 us in 13 chunks a
+// layer, 103 in 16).
 constexpr int kTargetChunks = 512, kCus = 256;
 int64_t chunks_for(int32_t L, int64_t keys) {
     const int64_t least = std::max<int64_t>(std::max(1, kTargetChunks / L), (keys + kMostKeys - 1) / kMostKeys);
@@ -443,14 +453,14 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
     a.ml = reinterpret_cast<float2*>(a.part + rows * D);
     a.parts = reinterpret_cast<uint32_t*>(a.ml + rows);
     if (!RAG && v.ev) {
-        a.least = reinterpret_cast<uint64_t*>(a.parts + static_cast<size_t>(v.L) * v.Hkv * 7 * kMostProducts * vz::kWave);
+        a.least = reinterpret_cast<uint64_t*>(a.parts + static_cast<size_t>(v.L) * v.Hkv * query_words(D, PACK));
         a.ev_budget = v.ev_budget;
         a.ev_sink = v.ev_sink;
         a.ev_M = v.ev_M;
     }
-    static_assert(Queries<DT, D, PACK>::kProducts <= kMostProducts, "room in the workspace");
-    const int chunks = RAG ? a.nc_max : a.n_chunks;
-    hipLaunchKernelGGL((stats_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L, (a.Hkv * a.shares + kWaves - 1) / kWaves), dim3(kThreads), 0, stream, a);
+    static_assert(Queries<DT, D, PACK>::kWords <= query_words(D, PACK), "room in the workspace");
+    const int chunks = RAG ? a.nc_max : a.n_chunks, groups = (a.Hkv * a.shares + kWaves - 1) / kWaves;
+    hipLaunchKernelGGL((stats_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L, groups), dim3(kThreads), 0, stream, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((values_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L), dim3(kThreads), 0, stream, a);
@@ -466,7 +476,7 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
 
 template <int DT, int D>
 hipError_t launch_any(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream) {
-    const bool pack = v.Hq / v.Hkv <= 8;
+    const bool pack = packs(v.Hq, v.Hkv);
     if (v.rag.n > 0) return pack ? launch<DT, D, true, true>(v, c, stream) : launch<DT, D, true, false>(v, c, stream);
     return pack ? launch<DT, D, false, true>(v, c, stream) : launch<DT, D, false, false>(v, c, stream);
 }
@@ -475,9 +485,9 @@ hipError_t launch_any(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t str
 
 size_t vz_decode_q4_ws_bytes(int32_t L, int32_t Hq, int32_t Hkv, int32_t d, int64_t plane, int32_t n_seqs) {
     const size_t rows = static_cast<size_t>(L) * chunk_rows(L, plane, n_seqs) * shares_of(Hkv) * Hq;
-    const size_t queries = static_cast<size_t>(std::max(n_seqs, 1)) * L * Hkv;
+    const size_t queries = static_cast<size_t>(std::max(n_seqs, 1)) * L * Hkv * query_words(d, packs(Hq, Hkv));
     const size_t least = n_seqs > 0 ? 0 : static_cast<size_t>(L) * chunk_rows(L, plane, 0) * 2 * sizeof(uint64_t);
-    return rows * (d * sizeof(float) + sizeof(float2)) + queries * 7 * kMostProducts * vz::kWave * sizeof(uint32_t) + least;
+    return rows * (d * sizeof(float) + sizeof(float2)) + queries * sizeof(uint32_t) + least;
 }
 
 bool vz_decode_q4_evicts(const VzDecodeArgs& a, int32_t budget, bool kept) { return !kept && a.len == budget; }

@@ -8,6 +8,7 @@
 
 #include "evict_args.h"
 #include "q4.h"
+#include "q4_calls.h"
 
 namespace {
 
@@ -21,8 +22,8 @@ __device__ __forceinline__ int64_t move_pieces(int n, int Hkv) {
     return static_cast<int64_t>(n) * Hkv * 2 * (vz_q4::Rows<D>::kCodes / 16 + 1);
 }
 template <int D>
-__device__ __forceinline__ void move_piece(const VzQ4Cache& c, size_t base, size_t head_rows, int Hkv, const int32_t* src,
-                                           const int32_t* dst, int64_t i) {
+__device__ __forceinline__ void move_piece(const VzQ4Cache& c, size_t base, size_t head_rows, int Hkv,
+                                           const int32_t* src, const int32_t* dst, int64_t i) {
     using R = vz_q4::Rows<D>;
     constexpr int CH = R::kCodes / 16, PIECES = CH + 1;
     const int p = static_cast<int>(i % PIECES);
@@ -59,9 +60,9 @@ __device__ void evict_layer(const SelJob<uint16_t>& job, const VzQ4Cache& c, siz
 }
 
 template <int D, bool LK>
-__global__ __launch_bounds__(kSel) void select_q4_kernel(const VzEvictArgs a, const VzQ4Cache c, int32_t* __restrict__ ws_n,
-                                                         int32_t* __restrict__ ws_src, int32_t* __restrict__ ws_dst,
-                                                         int inline_kv) {
+__global__ __launch_bounds__(kSel) void select_q4_kernel(const VzEvictArgs a, const VzQ4Cache c,
+                                                         int32_t* __restrict__ ws_n, int32_t* __restrict__ ws_src,
+                                                         int32_t* __restrict__ ws_dst, int inline_kv) {
     __shared__ SelSh<LK> sh;
     const int l = blockIdx.x;
     const size_t row = static_cast<size_t>(l) * a.cap;
@@ -84,7 +85,8 @@ __global__ __launch_bounds__(kSel) void select_q4_kernel(const VzEvictArgs a, co
 
 template <int D>
 __global__ __launch_bounds__(kSel) void select_q4_ragged_kernel(const VzEvictArgs a, const VzQ4Cache c,
-                                                                int32_t* __restrict__ ws_n, int32_t* __restrict__ ws_src,
+                                                                int32_t* __restrict__ ws_n,
+                                                                int32_t* __restrict__ ws_src,
                                                                 int32_t* __restrict__ ws_dst) {
     __shared__ SelSh<true> sh;
     const int l = blockIdx.x, s = blockIdx.y;

@@ -22,6 +22,7 @@
 
 #include "fuse_args.h"
 #include "q4.h"
+#include "q4_calls.h"
 
 namespace {
 
