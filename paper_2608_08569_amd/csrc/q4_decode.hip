@@ -326,18 +326,20 @@ __global__ __launch_bounds__(kThreads, DT == VZ_F32 && D == 128 && !PACK ? 2 : 3
     }
 }
 
-// Four-element pieces of a sequence's output rows per thread; blocks per (layer, sequence).
-__host__ __device__ inline int out_blocks(int Hq, int D) { return (Hq * D / 4 + kThreads - 1) / kThreads; }
+// Four-element pieces of a sequence's output rows: `groups` threads of a block
+// each add up a part of a piece's chunks.  Blocks per (layer, sequence).
+__host__ __device__ inline int out_blocks(int Hq, int D, int groups) {
+    return (Hq * D / 4 * groups + kThreads - 1) / kThreads;
+}
 
-// Blocks [0, out_blocks x sequences) of a layer: output rows from the chunks',
-// thread = four elements; in a ragged call the sequence's status too.  A block
-// after them, where one slot is evicted: the slot past the budget fills the one
-// with the smallest key.
-template <int DT, int D, bool RAG>
+// Blocks [0, out_blocks x sequences) of a layer: output rows from the chunks';
+// in a ragged call the sequence's status too.  A block after them, where one
+// slot is evicted: the slot past the budget fills the one with the smallest key.
+template <int DT, int D, bool RAG, int GROUPS>
 __global__ __launch_bounds__(kThreads) void finish_kernel(const Q4Args a) {
     using R = Rows<D>;
     using T = typename vz::Elem<DT>::T;
-    const int l = blockIdx.y, t = threadIdx.x, blocks = out_blocks(a.Hq, D);
+    const int l = blockIdx.y, t = threadIdx.x, blocks = out_blocks(a.Hq, D, GROUPS);
     const int s = blockIdx.x / blocks, part = blockIdx.x - s * blocks;
     if (!RAG && s > 0) {
         __shared__ uint64_t s_least[kWaves];
@@ -392,18 +394,32 @@ __global__ __launch_bounds__(kThreads) void finish_kernel(const Q4Args a) {
             a.rag.status[s] = ok ? VZ_OK : (st != VZ_OK ? st : VZ_ERR_CAPACITY);
         if (!ok) return;
     }
-    const int rows = nc * a.shares, n = a.Hq * D, e = 4 * (part * kThreads + t);
-    if (rows == 1 || e >= n) return;
-    const float* const p = part_of(a, l, first, 0, 0, D) + e;
+    const int rows = nc * a.shares, n = a.Hq * D;
+    if (rows == 1) return;
+    constexpr int PIECES = kThreads / GROUPS;
+    const int group = t / PIECES, e = 4 * (part * PIECES + t % PIECES);
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int r = 0; r < rows; ++r) {
-        const float4 x = *reinterpret_cast<const float4*>(p + static_cast<size_t>(r) * n);
+    auto add = [&](const float4& x) {
         o.x += x.x;
         o.y += x.y;
         o.z += x.z;
         o.w += x.w;
+    };
+    if (e < n) {
+        const float* const p = part_of(a, l, first, 0, 0, D) + e;
+#pragma unroll 8
+        for (int r = group; r < rows; r += GROUPS)
+            add(*reinterpret_cast<const float4*>(p + static_cast<size_t>(r) * n));
     }
+    if constexpr (GROUPS > 1) {
+        __shared__ float4 s_part[GROUPS][PIECES];
+        s_part[group][t % PIECES] = o;
+        __syncthreads();
+        if (group == 0)
+#pragma unroll
+            for (int r = 1; r < GROUPS; ++r) add(s_part[r][t]);
+    }
+    if (group != 0 || e >= n) return;
     T* const dst = static_cast<T*>(a.out) + (static_cast<size_t>(s) * a.L + l) * n + e;
     dst[0] = vz::Elem<DT>::from_f32(o.x);
     dst[1] = vz::Elem<DT>::from_f32(o.y);
@@ -430,24 +446,43 @@ int64_t chunks_for(int32_t L, int64_t keys) {
     const int64_t least = std::max<int64_t>(std::max(1, kTargetChunks / L), (keys + kMostKeys - 1) / kMostKeys);
     return (least * L + kCus - 1) / kCus * kCus / L;
 }
-// Keys per chunk, a multiple of 32.
-int chunk_for(int32_t L, int64_t keys) {
-    const int64_t chunks = chunks_for(L, keys), even = (keys + chunks - 1) / chunks;
-    return static_cast<int>((even + kUnit - 1) / kUnit * kUnit);
+// Keys per chunk: a multiple of what its waves take at a time, so that none of
+// them leaves an empty pair and row to be read (one layer of 4401 slots, one KV
+// head: 45 us in chunks of 32 keys, 20 in chunks of 128).
+int chunk_for(int32_t L, int32_t Hkv, int64_t keys) {
+    const int64_t chunks = chunks_for(L, keys), even = (keys + chunks - 1) / chunks, step = kUnit * shares_of(Hkv);
+    return static_cast<int>((even + step - 1) / step * step);
 }
 // Chunk rows per layer that a workspace for planes of `plane` slots holds: a
 // ragged call's; a single sequence's of any length up to the plane's.
-int64_t chunk_rows(int32_t L, int64_t plane, int32_t n_seqs) {
-    if (n_seqs > 0) return plane / chunk_for(L, plane) + n_seqs;
-    return std::min<int64_t>((plane + kUnit - 1) / kUnit, chunks_for(L, plane));
+int64_t chunk_rows(int32_t L, int32_t Hkv, int64_t plane, int32_t n_seqs) {
+    if (n_seqs > 0) return plane / chunk_for(L, Hkv, plane) + n_seqs;
+    const int step = kUnit * shares_of(Hkv);
+    return std::min<int64_t>((plane + step - 1) / step, chunks_for(L, plane));
+}
+
+// Threads per piece of the output rows: four where a thread each leaves CUs
+// empty (one layer of 4401 slots on one KV head: the step takes 15 us for 20; 48
+// layers of 8193: 72 for 74), one where the rows fill the GPU (48 layers of a
+// batch of eight: 245 us for 248).
+constexpr int kFewBlocks = 512;
+template <int DT, int D, bool RAG, int GROUPS>
+hipError_t launch_finish(const Q4Args& a, hipStream_t stream) {
+    const int blocks = out_blocks(a.Hq, D, GROUPS);
+    const int outs = RAG ? blocks * a.rag.n : a.n_chunks * a.shares > 1 ? blocks : 0;
+    // (the evicting block is found by its place behind the output blocks)
+    const int grid = a.ev_budget > 0 ? blocks + 1 : outs;
+    if (grid == 0) return hipSuccess;
+    hipLaunchKernelGGL((finish_kernel<DT, D, RAG, GROUPS>), dim3(grid, a.L), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
 }
 
 template <int DT, int D, bool RAG, bool PACK>
 hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream) {
     Q4Args a{};
     const int64_t plane = RAG ? v.rag.total : v.cap;
-    static_cast<AttendArgs&>(a) = attend_args(v, c, static_cast<int32_t>(chunk_rows(v.L, plane, v.rag.n)),
-                                              chunk_for(v.L, RAG ? plane : v.len + 1));
+    static_cast<AttendArgs&>(a) = attend_args(v, c, static_cast<int32_t>(chunk_rows(v.L, v.Hkv, plane, v.rag.n)),
+                                              chunk_for(v.L, v.Hkv, RAG ? plane : v.len + 1));
     const size_t rows = static_cast<size_t>(v.L) * a.nc_max * a.shares * v.Hq;
     a.part = static_cast<float*>(v.ws);
     a.ml = reinterpret_cast<float2*>(a.part + rows * D);
@@ -465,13 +500,10 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((values_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L), dim3(kThreads), 0, stream, a);
     e = hipGetLastError();
-    const int outs = RAG || chunks * a.shares > 1 ? out_blocks(a.Hq, D) * (RAG ? v.rag.n : 1) : 0;
-    const int evicts = a.ev_budget > 0 ? 1 : 0;
-    if (e != hipSuccess || outs + evicts == 0) return e;
-    // (the evicting block is found by its place behind the output blocks)
-    const int blocks = evicts ? out_blocks(a.Hq, D) + 1 : outs;
-    hipLaunchKernelGGL((finish_kernel<DT, D, RAG>), dim3(blocks, a.L), dim3(kThreads), 0, stream, a);
-    return hipGetLastError();
+    if (e != hipSuccess) return e;
+    return static_cast<int64_t>(out_blocks(a.Hq, D, 1)) * (RAG ? v.rag.n : 1) * a.L < kFewBlocks
+               ? launch_finish<DT, D, RAG, 4>(a, stream)
+               : launch_finish<DT, D, RAG, 1>(a, stream);
 }
 
 template <int DT, int D>
@@ -484,9 +516,9 @@ hipError_t launch_any(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t str
 }  // namespace
 
 size_t vz_decode_q4_ws_bytes(int32_t L, int32_t Hq, int32_t Hkv, int32_t d, int64_t plane, int32_t n_seqs) {
-    const size_t rows = static_cast<size_t>(L) * chunk_rows(L, plane, n_seqs) * shares_of(Hkv) * Hq;
+    const size_t rows = static_cast<size_t>(L) * chunk_rows(L, Hkv, plane, n_seqs) * shares_of(Hkv) * Hq;
     const size_t queries = static_cast<size_t>(std::max(n_seqs, 1)) * L * Hkv * query_words(d, packs(Hq, Hkv));
-    const size_t least = n_seqs > 0 ? 0 : static_cast<size_t>(L) * chunk_rows(L, plane, 0) * 2 * sizeof(uint64_t);
+    const size_t least = n_seqs > 0 ? 0 : static_cast<size_t>(L) * chunk_rows(L, Hkv, plane, 0) * 2 * sizeof(uint64_t);
     return rows * (d * sizeof(float) + sizeof(float2)) + queries * sizeof(uint32_t) + least;
 }
 

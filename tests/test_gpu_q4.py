@@ -273,6 +273,20 @@ def test_decode_of_many_chunks_and_layers(dtype, d, Hq, Hkv, L, length):
     run_single(Case(3, L, Hq, Hkv, d, length + 1, dtype), length, length, 0.9, L)
 
 
+@pytest.mark.parametrize("more", [-32, -1, 0, 1])
+@pytest.mark.parametrize("dtype,d,Hq,Hkv", SHAPES + [(BF16, 128, 16, 16), (F32, 128, 12, 12), (BF16, 64, 17, 17)])
+def test_decode_around_whole_units_of_keys(dtype, d, Hq, Hkv, more):
+    units = 140 // (Hkv * (1 if Hq // Hkv <= 8 else 2))
+    length = 32 * units - 1 + more
+    run_single(Case(length, 2, Hq, Hkv, d, length + 1, dtype), length, length, 0.95, 2)
+
+
+@pytest.mark.parametrize("length", [0, 1, 31, 32, 63])
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (F32, 64)])
+def test_short_caches_of_many_layers(dtype, d, length):
+    run_single(Case(length, 257, 2, 1, d, length + 1, dtype), length, length, 0.95, 257)
+
+
 @pytest.mark.parametrize("gamma,scale", [(0.0, 0.0), (1.0, 0.5), (0.5, 1e-3)])
 def test_decode_decay_and_scale(gamma, scale):
     run_single(Case(8, 2, 8, 2, 128, 300, BF16), 290, 300, gamma, 2, scale)
@@ -419,7 +433,9 @@ def test_ragged_evict_is_the_single_calls(d):
 # ---- together ----
 
 STEPS = [(BF16, 128, 32, 4, 1, 1024, 1024), (F32, 64, 4, 1, 2, 128, 128), (BF16, 64, 14, 2, 3, 300, 200),
-         (BF16, 128, 16, 1, 1, 50, 100), (F32, 128, 10, 5, 2, 700, 690), (BF16, 128, 8, 2, 40, 90, 90)]
+         (BF16, 128, 16, 1, 1, 50, 100), (F32, 128, 10, 5, 2, 700, 690), (BF16, 128, 8, 2, 40, 90, 90),
+         (BF16, 128, 32, 4, 1, 1300, 1300), (F32, 64, 4, 1, 2, 4600, 4600), (BF16, 64, 18, 2, 3, 2400, 2400),
+         (F32, 128, 10, 5, 2, 700, 700), (BF16, 64, 16, 16, 1, 200, 200), (BF16, 64, 2, 1, 257, 40, 40)]
 
 
 @pytest.mark.parametrize("kept", [False, True])
