@@ -435,22 +435,25 @@ constexpr int query_words(int d, bool pack) {
 // Groups of at most 8 heads take two parts of the queries a product.
 bool packs(int32_t Hq, int32_t Hkv) { return Hq / Hkv <= 8; }
 
-// Chunks per layer: kTargetChunks over the layers (two workgroups per CU: 8193
-// slots of 48 layers in 77 us, with three 81: each chunk costs its queries,
-// pairs and partial outputs, each missing one loads in flight), or what
-// kMostKeys asks for where that is more, and then as many as give every CU the
-// same number of workgroups (13,181 keys of 48 layers: 109 us in 13 chunks a
-// layer, 103 in 16).
-constexpr int kTargetChunks = 512, kCus = 256;
-int64_t chunks_for(int32_t L, int64_t keys) {
-    const int64_t least = std::max<int64_t>(std::max(1, kTargetChunks / L), (keys + kMostKeys - 1) / kMostKeys);
+// Chunks per layer: two workgroups per CU over the layers where a wave then has
+// two rounds of keys or more, else one (each costs its queries, pairs and
+// partial outputs: 24 layers of 4001 keys, d = 64, 19 us with two and 21 with
+// one; 48 layers of 300 keys 20 and 17; 48 layers of 8193 with three 81 for 77);
+// or what kMostKeys asks for where that is more, and then as many as give every
+// CU the same number (13,181 keys of 48 layers: 109 us in 13 chunks a layer, 103
+// in 16).
+constexpr int kCus = 256;
+int64_t chunks_for(int32_t L, int32_t Hkv, int64_t keys) {
+    const int64_t rounds = keys * L / (kUnit * shares_of(Hkv));
+    const int64_t target = rounds >= 2 * 2 * kCus ? 2 * kCus : kCus;
+    const int64_t least = std::max<int64_t>(std::max<int64_t>(1, target / L), (keys + kMostKeys - 1) / kMostKeys);
     return (least * L + kCus - 1) / kCus * kCus / L;
 }
 // Keys per chunk: a multiple of what its waves take at a time, so that none of
 // them leaves an empty pair and row to be read (one layer of 4401 slots, one KV
 // head: 45 us in chunks of 32 keys, 20 in chunks of 128).
 int chunk_for(int32_t L, int32_t Hkv, int64_t keys) {
-    const int64_t chunks = chunks_for(L, keys), even = (keys + chunks - 1) / chunks, step = kUnit * shares_of(Hkv);
+    const int64_t chunks = chunks_for(L, Hkv, keys), even = (keys + chunks - 1) / chunks, step = kUnit * shares_of(Hkv);
     return static_cast<int>((even + step - 1) / step * step);
 }
 // Chunk rows per layer that a workspace for planes of `plane` slots holds: a
@@ -458,7 +461,7 @@ int chunk_for(int32_t L, int32_t Hkv, int64_t keys) {
 int64_t chunk_rows(int32_t L, int32_t Hkv, int64_t plane, int32_t n_seqs) {
     if (n_seqs > 0) return plane / chunk_for(L, Hkv, plane) + n_seqs;
     const int step = kUnit * shares_of(Hkv);
-    return std::min<int64_t>((plane + step - 1) / step, chunks_for(L, plane));
+    return std::min<int64_t>((plane + step - 1) / step, chunks_for(L, Hkv, plane));
 }
 
 // Threads per piece of the output rows: four where a thread each leaves CUs
