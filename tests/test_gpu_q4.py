@@ -302,6 +302,57 @@ def test_one_part_of_the_keys_far_below_the_rest(dtype):
     run_single(c, 390, 390, 0.9, 2, scale=1.0, large_logits=True)
 
 
+@pytest.mark.parametrize("dtype,d,Hq,Hkv", [(BF16, 128, 8, 2), (F32, 64, 9, 1), (BF16, 64, 18, 2)])
+def test_a_query_that_is_not_finite_is_its_heads_alone(dtype, d, Hq, Hkv):
+    """Its outputs and its layer's scores are NaN; every other head's outputs keep their bits."""
+    m, t, n = vz(), torch(), 150
+    c = Case(7, 3, Hq, Hkv, d, n + 1, dtype)
+    q, kn, vn = (to_dev(x) for x in c.rows())
+    results = []
+    for bad in (False, True):
+        cache, s, p = c.dev()
+        if bad:
+            q[0, 1, 3], q[2, Hq - 1, d - 1] = float("inf"), float("nan")
+        out = t.zeros_like(q)
+        m.voxzip_decode_attend_score_q4(q, kn, vn, *cache, s, p, out, n, n, 0.9,
+                                        workspace=m.workspace(m.VZ_OP_DECODE_Q4, 3, Hq, Hkv, d, n + 1))
+        results.append((out, s, *cache))
+    (o0, s0, *c0), (o1, s1, *c1) = results
+    hit = t.zeros(3, Hq, dtype=t.bool, device="cuda")
+    hit[0, 1] = hit[2, Hq - 1] = True
+    assert o1[hit].isnan().all() and t.equal(o1[~hit], o0[~hit]) and not o0.isnan().any()
+    assert s1[[0, 2]].isnan().all() and t.equal(s1[1], s0[1])
+    assert all(t.equal(x, y) for x, y in zip(c0, c1))
+
+
+@pytest.mark.parametrize("dtype,d", [(BF16, 128), (BF16, 64), (F32, 128), (F32, 64)])
+def test_inputs_and_outputs_at_any_element_alignment(dtype, d):
+    m, t, L, Hq, Hkv, n = vz(), torch(), 2, 6, 2, 130
+    c = Case(17, L, Hq, Hkv, d, n + 1, dtype)
+    rows = [to_dev(x) for x in c.rows()]
+    k, v = (to_dev(store(c.rng.standard_normal((L, Hkv, 400, d)), dtype)) for _ in "kv")
+    ak, av = (to_dev(store(c.rng.standard_normal((L, Hkv, n, d)), dtype)) for _ in "kv")
+    off = i32(sorted(c.rng.choice(399, n - 1, replace=False) + 1))
+    off = t.cat([i32([0]), off, i32([400])])
+
+    def odd(x):
+        """The same values one element further on."""
+        y = t.empty(x.numel() + 1, dtype=x.dtype, device="cuda")[1:].view(x.shape)
+        y.copy_(x)
+        return y
+
+    results = []
+    for move in (lambda x: x, odd):
+        cache, s, p = m.q4_cache(L, Hkv, n + 1, d), t.zeros(L, n + 1, device="cuda"), i32([[0] * (n + 1)] * L)
+        m.voxzip_fuse_spans_q4(move(k), move(v), off, *cache, s, p, anchor_k=move(ak), anchor_v=move(av))
+        out = move(t.zeros_like(rows[0]))
+        m.voxzip_decode_attend_score_q4(*(move(x) for x in rows), *cache, s, p, out, n, n, 0.9,
+                                        workspace=m.workspace(m.VZ_OP_DECODE_Q4, L, Hq, Hkv, d, n + 1))
+        results.append((*cache, s, p, out))
+    for x, y in zip(*results):
+        assert t.equal(x, y)
+
+
 @pytest.mark.parametrize("dtype,d,Hq,Hkv,L", [(BF16, 128, 32, 4, 2), (F32, 64, 4, 1, 3), (BF16, 64, 18, 2, 1),
                                               (F32, 128, 10, 5, 1)])
 def test_ragged_decode_against_oracle(dtype, d, Hq, Hkv, L):
