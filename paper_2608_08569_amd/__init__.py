@@ -399,10 +399,13 @@ def _expect_q4(d, k_codes, k_scales, v_codes, v_scales):
         raise ValueError(f"head size must be 64 or 128, not {d}")
     if k_codes.dim() != 4:
         raise ValueError("k_codes must be [layers][heads][slots][d / 2]")
-    L, H, cap = k_codes.shape[:3]
-    u8, codes, scales = torch.uint8, (L, H, cap, d // 2), (L, H, cap, d // 32)
-    _expect_all(((k_codes, codes, "k_codes", u8), (k_scales, scales, "k_scales", u8), (v_codes, codes, "v_codes", u8),
-                 (v_scales, scales, "v_scales", u8)))
+    L, H, cap, width = k_codes.shape
+    u8, scales = torch.uint8, (L, H, cap, d // 32)
+    if (width != d // 2 or v_codes.shape != k_codes.shape or k_scales.shape != scales or v_scales.shape != scales
+            or not k_codes.dtype == k_scales.dtype == v_codes.dtype == v_scales.dtype == u8):  # which one, then
+        codes = (L, H, cap, d // 2)
+        _expect_all(((k_codes, codes, "k_codes", u8), (k_scales, scales, "k_scales", u8),
+                     (v_codes, codes, "v_codes", u8), (v_scales, scales, "v_scales", u8)))
     return L, H, cap
 
 
@@ -410,21 +413,16 @@ def _pointers(stream, *tensors):
     """Stream handle and pointers of a call whose tensors have to be contiguous
     and on the current device, whose stream the kernels are launched on."""
     import torch
-    device, out = tensors[0].get_device(), []
+    device = tensors[0].get_device()
     for t in tensors:
-        if t is None:
-            out.append(None)
-            continue
-        if t.get_device() != device:
-            raise ValueError("tensors must be on one device")
-        if not t.is_contiguous():
-            raise ValueError("tensors must be contiguous")
-        out.append(t.data_ptr())
+        if t is not None and (t.get_device() != device or not t.is_contiguous()):
+            raise ValueError(f"tensors must be {'on one device' if t.get_device() != device else 'contiguous'}")
     if device < 0:
         raise ValueError("tensors must be on the GPU")
     if device != torch.cuda.current_device():
         raise ValueError("tensors must be on the current device")
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream, out
+    return (torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream,
+            [None if t is None else t.data_ptr() for t in tensors])
 
 
 def voxzip_fuse_spans_q4(k_in, v_in, span_off, k_codes, k_scales, v_codes, v_scales, score_out, pos_out,
