@@ -281,7 +281,7 @@ __global__ __launch_bounds__(kThreads, DT == VZ_F32 && D == 128 && !PACK ? 2 : 3
             }
         }
         __syncthreads();
-        // the sums of this round's KV heads, in head order
+        // the sums of these KV heads, in head order
 #pragma unroll
         for (int i = 0; i < KEYS_PER_THREAD; ++i) {
             const int key = threadIdx.x + i * kThreads;

@@ -116,37 +116,33 @@ __device__ __forceinline__ void add_rows(const typename vz::Elem<DT>::T* __restr
 // than half a float32 step and 2^-48 of it away, and stays on its side.  (Not
 // where x / n may lie below the normal floats.)
 constexpr double kMostExact = 1 << 19;
+constexpr int kFuseThreads = 256;
+template <int DT, int D>
+constexpr int kSpansPerBlock = kFuseThreads / (D / vz::Elem<DT>::kPer16B);
+
+// The spans of one sequence, and where its rows begin in their planes.
+struct Spans {
+    int T_in, n_spans;
+    const int32_t* off;
+    int64_t in_row, out_row;
+};
+
+// One block's spans, number bx of its sequence's, in one plane.
 template <int DT, int D, bool RAG>
-__global__ __launch_bounds__(256) void fuse_q4_kernel(const FuseArgs a, const VzQ4Cache out) {
+__device__ __forceinline__ void fuse_block(const FuseArgs& a, const VzQ4Cache& out, const Spans& q, int bx, int l,
+                                           int h, int which, int thread) {
     using E = vz::Elem<DT>;
     using T = typename E::T;
     using R = vz_q4::Rows<D>;
     constexpr int PER = E::kPer16B;              // elements per 16-byte vector
     constexpr int LANES = D / PER;               // lanes per span row
-    constexpr int SPB = 256 / LANES;             // spans per block
     constexpr int BLANES = vz_q4::kBlock / PER;  // lanes per block of channels
-
-    const int sub = threadIdx.x / LANES;
-    const int lane = threadIdx.x % LANES;
-    const int which = blockIdx.y & 1;  // 0: K, 1: V
-    const int h = blockIdx.y >> 1;
-    const int l = blockIdx.z;
-    int bx = blockIdx.x, T_in = a.T_in, n_spans = a.n_spans;
-    int64_t in_row = 0, out_row = 0;  // first row of the sequence in its planes
-    const int32_t* off = a.off;
-    if constexpr (RAG) {
-        const int s = blockIdx.x / a.blocks_per_seq;
-        bx = blockIdx.x - s * a.blocks_per_seq;
-        const int st = vz_fuse::ragged_fuse_status(a, s);
-        if (a.status && bx == 0 && blockIdx.y == 0 && l == 0 && threadIdx.x == 0) a.status[s] = st;
-        if (st != VZ_OK) return;
-        T_in = a.T_in_s[s];
-        n_spans = a.n_spans_s[s];
-        in_row = a.in_base[s];
-        out_row = a.base[s];
-        off = a.off + a.off_base[s];
-    }
-    const int64_t j = static_cast<int64_t>(bx) * SPB + sub;
+    const int sub = thread / LANES;
+    const int lane = thread % LANES;
+    const int T_in = q.T_in, n_spans = q.n_spans;
+    const int64_t in_row = q.in_row, out_row = q.out_row;
+    const int32_t* const off = q.off;
+    const int64_t j = static_cast<int64_t>(bx) * kSpansPerBlock<DT, D> + sub;
     if (j >= n_spans) return;
 
     int32_t b = off[j], e = off[j + 1];
@@ -227,18 +223,86 @@ __global__ __launch_bounds__(256) void fuse_q4_kernel(const FuseArgs a, const Vz
     }
 }
 
+// Grid: (blocks, 2 x KV heads, layers); y: KV head, K or V.
+template <int DT, int D>
+__global__ __launch_bounds__(kFuseThreads) void fuse_q4_kernel(const FuseArgs a, const VzQ4Cache out) {
+    const Spans q{a.T_in, a.n_spans, a.off, 0, 0};
+    fuse_block<DT, D, false>(a, out, q, blockIdx.x, blockIdx.z, blockIdx.y >> 1, blockIdx.y & 1, threadIdx.x);
+}
+
+// A ragged batch, a workgroup for each block of spans that a sequence may have.
+template <int DT, int D>
+__global__ __launch_bounds__(kFuseThreads) void fuse_q4_ragged_kernel(const FuseArgs a, const VzQ4Cache out) {
+    const int l = blockIdx.z, s = blockIdx.x / a.blocks_per_seq, bx = blockIdx.x - s * a.blocks_per_seq;
+    const int st = vz_fuse::ragged_fuse_status(a, s);
+    if (a.status && bx == 0 && blockIdx.y == 0 && l == 0 && threadIdx.x == 0) a.status[s] = st;
+    if (st != VZ_OK) return;
+    const Spans q{a.T_in_s[s], a.n_spans_s[s], a.off + a.off_base[s], a.in_base[s], a.base[s]};
+    fuse_block<DT, D, true>(a, out, q, bx, l, blockIdx.y >> 1, blockIdx.y & 1, threadIdx.x);
+}
+
+// The same with as many workgroups as fill the GPU: a plane's blocks of spans
+// are numbered over its served sequences, and each workgroup takes every
+// gridDim.x-th.
+template <int DT, int D>
+__global__ __launch_bounds__(kFuseThreads, 7) void fuse_q4_batch_kernel(const FuseArgs a, const VzQ4Cache out) {
+    constexpr int SPB = kSpansPerBlock<DT, D>;
+    const int l = blockIdx.z, lane = threadIdx.x % vz::kWave;
+    if (a.status && blockIdx.x == 0 && blockIdx.y == 0 && l == 0)
+        for (int s = threadIdx.x; s < a.n_seqs; s += kFuseThreads) a.status[s] = vz_fuse::ragged_fuse_status(a, s);
+    // 64 sequences at a time, one per lane: their blocks, and those up to each
+    int s0 = 0, before = 0, blocks = 0, upto = 0;
+    auto count = [&] {
+        const int s = min(s0 + lane, a.n_seqs - 1);
+        const bool served = vz_fuse::ragged_fuse_status(a, s) == VZ_OK && s0 + lane < a.n_seqs;
+        blocks = served ? (a.n_spans_s[s] + SPB - 1) / SPB : 0;
+        upto = vz::wave_incl_scan(blocks);
+    };
+    count();
+    for (int f = blockIdx.x;; f += gridDim.x) {
+        while (f >= before + __builtin_amdgcn_readlane(upto, vz::kWave - 1)) {
+            before += __builtin_amdgcn_readlane(upto, vz::kWave - 1);
+            s0 += vz::kWave;
+            if (s0 >= a.n_seqs) return;
+            count();
+        }
+        const int src = __builtin_ctzll(__ballot(before + upto > f));
+        const int s = s0 + src;
+        const int bx = f - before - __builtin_amdgcn_readlane(upto, src) + __builtin_amdgcn_readlane(blocks, src);
+        const Spans q{a.T_in_s[s], a.n_spans_s[s], a.off + a.off_base[s], a.in_base[s], a.base[s]};
+        // (what a thread's number gives is formed again each time: over the loop it would take the loads' registers)
+        int thread = threadIdx.x;
+        asm volatile("" : "+v"(thread));
+        fuse_block<DT, D, true>(a, out, q, bx, l, blockIdx.y >> 1, blockIdx.y & 1, thread);
+    }
+}
+
+// A workgroup that finds no spans costs the time of its dispatch, and the host
+// knows no sequence's length.  Many of them outweigh what looking the blocks up
+// costs: 12 layers of 16 sequences of up to 9000 tokens (215,000 workgroups), all
+// but one of 10: 175 us with a workgroup for each, 67 with 8192; four of 2k-9k
+// (53,760): 128 and 129, four of 4938 114 and 129.
+constexpr int64_t kFuseMany = 65536, kFuseFill = 8192;
 template <int DT, int D>
 hipError_t launch(FuseArgs a, const VzQ4Cache& out, int32_t L, hipStream_t stream) {
-    constexpr int SPB = 256 / (D / vz::Elem<DT>::kPer16B);
+    constexpr int SPB = kSpansPerBlock<DT, D>;
+    const int planes = 2 * a.H;
     if (a.n_seqs > 0) {
         a.blocks_per_seq = std::max(1, (a.max_spans + SPB - 1) / SPB);  // at least one reports the status
-        const dim3 grid(static_cast<unsigned>(static_cast<int64_t>(a.blocks_per_seq) * a.n_seqs), 2 * a.H, L);
-        hipLaunchKernelGGL((fuse_q4_kernel<DT, D, true>), grid, dim3(256), 0, stream, a, out);
+        const int64_t blocks = static_cast<int64_t>(a.blocks_per_seq) * a.n_seqs, all = blocks * planes * L;
+        if (all <= kFuseMany) {
+            const dim3 grid(static_cast<unsigned>(blocks), planes, L);
+            hipLaunchKernelGGL((fuse_q4_ragged_kernel<DT, D>), grid, dim3(kFuseThreads), 0, stream, a, out);
+        } else {
+            const int64_t fill = std::max<int64_t>(1, kFuseFill / (static_cast<int64_t>(planes) * L));
+            const dim3 grid(static_cast<unsigned>(std::min(blocks, fill)), planes, L);
+            hipLaunchKernelGGL((fuse_q4_batch_kernel<DT, D>), grid, dim3(kFuseThreads), 0, stream, a, out);
+        }
         return hipGetLastError();
     }
     if (a.n_spans == 0) return hipSuccess;
-    const dim3 grid((a.n_spans + SPB - 1) / SPB, 2 * a.H, L);
-    hipLaunchKernelGGL((fuse_q4_kernel<DT, D, false>), grid, dim3(256), 0, stream, a, out);
+    const dim3 grid((a.n_spans + SPB - 1) / SPB, planes, L);
+    hipLaunchKernelGGL((fuse_q4_kernel<DT, D>), grid, dim3(kFuseThreads), 0, stream, a, out);
     return hipGetLastError();
 }
 

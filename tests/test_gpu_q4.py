@@ -226,6 +226,47 @@ def test_ragged_fusion_is_the_single_calls(dtype, d):
     assert (from_dev(s)[:, free] == 7).all() and (from_dev(p)[:, free] == -7).all()
 
 
+@pytest.mark.parametrize("n,dtype,d,H", [(5, F32, 64, 2), (63, BF16, 64, 2), (64, BF16, 128, 6), (65, F32, 64, 5),
+                                         (200, BF16, 64, 2), (200, F32, 128, 3)])
+def test_ragged_fusion_of_many_sequences(n, dtype, d, H):
+    """Lengths from one row to thousands, idle slots and refused sequences between them."""
+    m, t, L = vz(), torch(), 1
+    rng = np.random.default_rng(n)
+    T = np.where(rng.random(n) < 0.1, 2500, rng.integers(1, 60, n))
+    T[-1] = 3000
+    spans = np.maximum(1, T // rng.integers(1, 5, n))
+    cap = spans + rng.integers(0, 3, n)
+    idle, wrong = rng.random(n) < 0.2, rng.random(n) < 0.1
+    idle[-1] = wrong[-1] = False
+    offs = [np.concatenate([[0], np.sort(rng.choice(a - 1, b - 1, replace=False) + 1), [a]]) for a, b in zip(T, spans)]
+    ahead = lambda x: np.concatenate([[0], np.cumsum(x)[:-1]])
+    base, in_base, off_base = ahead(cap), ahead(T), ahead(spans + 1)
+    K, V = (store(rng.standard_normal((L, H, T.sum(), d)), dtype) for _ in "kv")
+    total = int(cap.sum())
+    cache = m.q4_cache(L, H, total, d)
+    for x in cache:
+        x.fill_(0x5A)
+    s, p = t.full((L, total), 7.0, device="cuda"), i32([[-7] * total] * L)
+    st = i32([99] * n)
+    m.voxzip_fuse_spans_q4_ragged(to_dev(K), to_dev(V), i64(in_base.tolist()), i32(T.tolist()),
+                                  i32(np.concatenate(offs).tolist()), i64(off_base.tolist()),
+                                  i32(np.where(wrong, T + 1, spans).tolist()), int(spans.max()), *cache, s, p,
+                                  i64(base.tolist()), i32(np.where(idle, 0, cap).tolist()), status=st)
+    assert from_dev(st).tolist() == [m.VZ_IDLE if i else m.VZ_ERR_SHAPE if w else m.VZ_OK for i, w in zip(idle, wrong)]
+    free = np.ones(total, dtype=bool)
+    got = [from_dev(x) for x in cache]
+    for i in np.flatnonzero(~idle & ~wrong):
+        at, rows = slice(base[i], base[i] + spans[i]), slice(in_base[i], in_base[i] + T[i])
+        want = sum((q4ref.span_means(widen(x[:, :, rows], dtype), offs[i]) for x in (K, V)), ())
+        for x, y, name in zip(got, want, NAMES):
+            assert np.array_equal(x[:, :, at], y), (i, name)
+        assert (from_dev(p)[:, at] == np.arange(spans[i])).all() and not from_dev(s)[:, at].any()
+        free[at] = False
+    for x in got:
+        assert (x[:, :, free] == 0x5A).all()
+    assert (from_dev(s)[:, free] == 7).all() and (from_dev(p)[:, free] == -7).all()
+
+
 # ---- decode ----
 
 SHAPES = [(BF16, 128, 32, 4), (F32, 128, 6, 3), (BF16, 64, 14, 2), (F32, 64, 4, 1), (BF16, 128, 16, 1),
