@@ -435,40 +435,49 @@ constexpr int query_words(int d, bool pack) {
 // Groups of at most 8 heads take two parts of the queries a product.
 bool packs(int32_t Hq, int32_t Hkv) { return Hq / Hkv <= 8; }
 
-// Chunks per layer: two workgroups per CU over the layers where a wave then has
-// two rounds of keys or more, else one (each costs its queries, pairs and
-// partial outputs: 24 layers of 4001 keys, d = 64, 19 us with two and 21 with
-// one; 48 layers of 300 keys 20 and 17; 48 layers of 8193 with three 81 for 77);
-// or what kMostKeys asks for where that is more, and then as many as give every
-// CU the same number (13,181 keys of 48 layers: 109 us in 13 chunks a layer, 103
-// in 16).
+// Chunks per layer:
+// - two workgroups per CU over the layers where a wave then has two rounds of
+//   keys or more, else one (each costs its queries, pairs and partial outputs: 24
+//   layers of 4001 keys, d = 64, 19 us with two and 21 with one; 48 layers of 300
+//   keys 20 and 17; 48 layers of 8193 with three 81 for 77);
+// - but no more than sqrt(1.4 keys / shares): a wave's keys, keys / (chunks x
+//   shares), and a sequence's pairs and rows, chunks x shares, are both gone
+//   through one after the other (one layer of 8001 keys on 4 KV heads: 20.5 us
+//   in 251 chunks, 15.2 in 84; on 8: 28 and 21; 16,001 keys on one: 27 and 18.5);
+// - no fewer than kMostKeys asks for;
+// - where that gives every CU one, as many as give each the same number (13,181
+//   keys of 48 layers: 109 us in 13 chunks a layer, 103 in 16).
 constexpr int kCus = 256;
-int64_t chunks_for(int32_t L, int32_t Hkv, int64_t keys) {
+int64_t chunks_for(int32_t L, int32_t Hkv, int64_t keys, int32_t n_seqs) {
     const int64_t rounds = keys * L / (kUnit * shares_of(Hkv));
-    const int64_t target = rounds >= 2 * 2 * kCus ? 2 * kCus : kCus;
-    const int64_t least = std::max<int64_t>(std::max<int64_t>(1, target / L), (keys + kMostKeys - 1) / kMostKeys);
-    return (least * L + kCus - 1) / kCus * kCus / L;
+    const int64_t target = (rounds >= 2 * 2 * kCus ? 2 * kCus : kCus) / L;
+    const double few = sqrt(1.4 * static_cast<double>(keys) * std::max(n_seqs, 1) / shares_of(Hkv));
+    const int64_t need = std::max<int64_t>(1, (keys + kMostKeys - 1) / kMostKeys);
+    const int64_t least = std::max(std::min(target, static_cast<int64_t>(few)), need);
+    return least * L < kCus ? least : (least * L + kCus - 1) / kCus * kCus / L;
 }
 // Keys per chunk: a multiple of what its waves take at a time, so that none of
 // them leaves an empty pair and row to be read (one layer of 4401 slots, one KV
 // head: 45 us in chunks of 32 keys, 20 in chunks of 128).
-int chunk_for(int32_t L, int32_t Hkv, int64_t keys) {
-    const int64_t chunks = chunks_for(L, Hkv, keys), even = (keys + chunks - 1) / chunks, step = kUnit * shares_of(Hkv);
+int chunk_for(int32_t L, int32_t Hkv, int64_t keys, int32_t n_seqs) {
+    const int64_t chunks = chunks_for(L, Hkv, keys, n_seqs), even = (keys + chunks - 1) / chunks;
+    const int64_t step = kUnit * shares_of(Hkv);
     return static_cast<int>((even + step - 1) / step * step);
 }
 // Chunk rows per layer that a workspace for planes of `plane` slots holds: a
 // ragged call's; a single sequence's of any length up to the plane's.
 int64_t chunk_rows(int32_t L, int32_t Hkv, int64_t plane, int32_t n_seqs) {
-    if (n_seqs > 0) return plane / chunk_for(L, Hkv, plane) + n_seqs;
+    if (n_seqs > 0) return plane / chunk_for(L, Hkv, plane, n_seqs) + n_seqs;
     const int step = kUnit * shares_of(Hkv);
-    return std::min<int64_t>((plane + step - 1) / step, chunks_for(L, Hkv, plane));
+    return std::min<int64_t>((plane + step - 1) / step, chunks_for(L, Hkv, plane, n_seqs));
 }
 
-// Threads per piece of the output rows: four where a thread each leaves CUs
-// empty (one layer of 4401 slots on one KV head: the step takes 15 us for 20; 48
-// layers of 8193: 72 for 74), one where the rows fill the GPU (48 layers of a
-// batch of eight: 245 us for 248).
-constexpr int kFewBlocks = 512;
+// Threads per piece of the output rows, by the workgroups that a thread each
+// makes: eight where those are next to none (one layer of 8001 keys on 4 KV
+// heads: the step takes 15 us, with four 16), four where they leave CUs empty (48
+// layers of 8193: 72 us, 74 with one, 72.5 with eight), one where they fill the
+// GPU (48 layers of a batch of eight: 245 us, 248 with four).
+constexpr int kFewBlocks = 512, kVeryFewBlocks = 64;
 template <int DT, int D, bool RAG, int GROUPS>
 hipError_t launch_finish(const Q4Args& a, hipStream_t stream) {
     const int blocks = out_blocks(a.Hq, D, GROUPS);
@@ -485,7 +494,7 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
     Q4Args a{};
     const int64_t plane = RAG ? v.rag.total : v.cap;
     static_cast<AttendArgs&>(a) = attend_args(v, c, static_cast<int32_t>(chunk_rows(v.L, v.Hkv, plane, v.rag.n)),
-                                              chunk_for(v.L, v.Hkv, RAG ? plane : v.len + 1));
+                                              chunk_for(v.L, v.Hkv, RAG ? plane : v.len + 1, v.rag.n));
     const size_t rows = static_cast<size_t>(v.L) * a.nc_max * a.shares * v.Hq;
     a.part = static_cast<float*>(v.ws);
     a.ml = reinterpret_cast<float2*>(a.part + rows * D);
@@ -504,9 +513,10 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
     hipLaunchKernelGGL((values_kernel<DT, D, RAG, PACK>), dim3(chunks, a.L), dim3(kThreads), 0, stream, a);
     e = hipGetLastError();
     if (e != hipSuccess) return e;
-    return static_cast<int64_t>(out_blocks(a.Hq, D, 1)) * (RAG ? v.rag.n : 1) * a.L < kFewBlocks
-               ? launch_finish<DT, D, RAG, 4>(a, stream)
-               : launch_finish<DT, D, RAG, 1>(a, stream);
+    const int64_t blocks = static_cast<int64_t>(out_blocks(a.Hq, D, 1)) * (RAG ? v.rag.n : 1) * a.L;
+    if (blocks < kVeryFewBlocks) return launch_finish<DT, D, RAG, 8>(a, stream);
+    if (blocks < kFewBlocks) return launch_finish<DT, D, RAG, 4>(a, stream);
+    return launch_finish<DT, D, RAG, 1>(a, stream);
 }
 
 template <int DT, int D>
