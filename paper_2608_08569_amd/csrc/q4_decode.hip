@@ -473,11 +473,12 @@ int64_t chunk_rows(int32_t L, int32_t Hkv, int64_t plane, int32_t n_seqs) {
 }
 
 // Threads per piece of the output rows, by the workgroups that a thread each
-// makes: eight where those are next to none (one layer of 8001 keys on 4 KV
-// heads: the step takes 15 us, with four 16), four where they leave CUs empty (48
-// layers of 8193: 72 us, 74 with one, 72.5 with eight), one where they fill the
-// GPU (48 layers of a batch of eight: 245 us, 248 with four).
-constexpr int kFewBlocks = 512, kVeryFewBlocks = 64;
+// makes: four where they leave CUs empty (48 layers of 8193: the step takes 72 us,
+// 74 with one, 72.5 with eight), eight where they are next to none and the rows
+// many (one layer of 8001 keys on 4 KV heads: 15 us, with four 16; but of 1025
+// keys, 33 rows, 13.3 and 12.3), one where they fill the GPU (48 layers of a
+// batch of eight: 245 us, 248 with four).
+constexpr int kFewBlocks = 512, kVeryFewBlocks = 64, kManyRows = 64;
 template <int DT, int D, bool RAG, int GROUPS>
 hipError_t launch_finish(const Q4Args& a, hipStream_t stream) {
     const int blocks = out_blocks(a.Hq, D, GROUPS);
@@ -514,7 +515,8 @@ hipError_t launch(const VzDecodeArgs& v, const VzQ4Cache& c, hipStream_t stream)
     e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t blocks = static_cast<int64_t>(out_blocks(a.Hq, D, 1)) * (RAG ? v.rag.n : 1) * a.L;
-    if (blocks < kVeryFewBlocks) return launch_finish<DT, D, RAG, 8>(a, stream);
+    const int of_one = chunks * a.shares / (RAG ? v.rag.n : 1);  // rows of a sequence
+    if (blocks < kVeryFewBlocks && of_one >= kManyRows) return launch_finish<DT, D, RAG, 8>(a, stream);
     if (blocks < kFewBlocks) return launch_finish<DT, D, RAG, 4>(a, stream);
     return launch_finish<DT, D, RAG, 1>(a, stream);
 }

@@ -50,7 +50,9 @@ class DecodeLoop:
     ``bits=4`` keeps the cache as 4-bit rows (``planes``: k_codes, k_scales,
     v_codes, v_scales, see :func:`q4_cache`) instead of ``k`` and ``v``
     (``planes``: k, v), in 3.76 times fewer bytes than bfloat16; prefills,
-    new rows, queries and outputs stay in ``dtype``.
+    new rows, queries and outputs stay in ``dtype``.  A request's rows are
+    then those it would have alone bit for bit, its outputs and scores to
+    float32 rounding.
     """
 
     NEVER = 1 << 30  # budget of a sequence whose eviction is not due this step
