@@ -96,7 +96,10 @@ __global__ __launch_bounds__(kThreads, 4) void stats_kernel(const Q4Args a) {
         const int u_new = (it.len - c0) / kUnit;
         const bool mine = newest && u_new % shares == share;
         if (mine) append<DT, D>(a, lane, row_g, head + it.len, s_new[w]);
-        float m = -INFINITY, ref = 0.f, z = 0.f;
+        // the largest logit, the same scaled, and the sum of exp2 relative to it.  While no key has a finite logit the
+        // scaled one is -inf, and the first that has one takes the empty sum by a factor of 0: by exp2 from any finite
+        // start it would be infinity times 0 where the logits lie far below it.
+        float m = -INFINITY, top = -INFINITY, z = 0.f;
         auto unit = [&](int i, KTile& k) {
             const int k0 = unit_key(i);
             if (mine && k0 + kUnit > it.len) put_new_k<D>(k, lane, it.len - k0, s_new[w]);
@@ -105,8 +108,9 @@ __global__ __launch_bounds__(kThreads, 4) void stats_kernel(const Q4Args a) {
             load_k<D>(k, lane, kc, ks, unit_key(i + kStatsDepth), old);  // (past the chunk: nothing)
             m = fmaxf(m, fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[0][2], x[0][3])));
             if constexpr (!PACK) m = fmaxf(m, fmaxf(fmaxf(x[1][0], x[1][1]), fmaxf(x[1][2], x[1][3])));
-            const float last = ref;
-            ref = finite_ref(m) * a.scale_log2;
+            const float last = top;
+            top = m * a.scale_log2;
+            const float ref = finite_ref(top);
             z *= __builtin_amdgcn_exp2f(last - ref);
 #pragma unroll
             for (int t = 0; t < (PACK ? 1 : 2); ++t)
@@ -119,10 +123,9 @@ __global__ __launch_bounds__(kThreads, 4) void stats_kernel(const Q4Args a) {
                 if (i + u < n_units) unit(i + u, kt[u]);
         }
         // the lanes that hold a head: exp2 relative to the largest of their references
-        m = m == -INFINITY ? -INFINITY : ref;
-        float mw = vz::rows_max(m);
+        float mw = vz::rows_max(top);
         if constexpr (PACK) mw = fmaxf(mw, vz::ror16<8>(mw));
-        z *= __builtin_amdgcn_exp2f(m - finite_ref(mw));
+        z *= __builtin_amdgcn_exp2f(top - finite_ref(mw));
         z = vz::rows_sum(z);
         if constexpr (PACK) z += vz::ror16<8>(z);
         if (q4 == 0 && r16 < G) ml_of(a, l, g * G + r16, it.first + c)[share] = make_float2(mw, z);
