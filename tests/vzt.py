@@ -47,7 +47,7 @@ def check_close(got: np.ndarray, ref: np.ndarray, rtol: float, what: str = "") -
     allow = rtol * np.abs(ref) + rtol * rms + 1e-30
     err = np.abs(got - ref)
     worst = float(np.max(err / allow))
-    if worst > 1.0:
+    if not worst <= 1.0:  # (a NaN is not)
         idx = np.unravel_index(np.argmax(err / allow), err.shape)
         raise AssertionError(f"{what}: element {idx} got {got[idx]!r} ref {ref[idx]!r} "
                              f"(err {err[idx]:.3g}, allowed {allow[idx]:.3g})")
@@ -67,7 +67,7 @@ def check_rel(got: np.ndarray, ref: np.ndarray, rtol: float, what: str = "") -> 
     allow = rtol * np.abs(ref) + 1e-38
     err = np.abs(got - ref)
     worst = float(np.max(err / allow))
-    if worst > 1.0:
+    if not worst <= 1.0:  # (a NaN is not)
         idx = np.unravel_index(np.argmax(err / allow), err.shape)
         raise AssertionError(f"{what}: element {idx} got {got[idx]!r} ref {ref[idx]!r} "
                              f"(err {err[idx]:.3g}, allowed {allow[idx]:.3g})")
