@@ -246,9 +246,14 @@ struct Queries {
         for (int p = 0; p < kParts; ++p) {
             const int ep = e - (p == 0 ? 0 : 5 * p - 1) + 127;
             const float scale = __uint_as_float(static_cast<uint32_t>(ep) << 23);
-            const u32x6 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(lo, hi, scale);
+            // Both conversions write registers before they have read all of their sources, and the compiler lets the
+            // two overlap (the last part came out wrong, float32 logits off by up to 2^-20 of a block's largest channel):
+            // the sources stay in use past them.
+            u32x6 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(lo, hi, scale);
+            asm volatile("" : "+v"(c) : "v"(lo), "v"(hi), "v"(scale));
             if (p + 1 < kParts) {
-                const f32x32 v = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(c, scale);
+                f32x32 v = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(c, scale);
+                asm volatile("" : "+v"(v) : "v"(c), "v"(scale));
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     lo[i] -= v[2 * i];
