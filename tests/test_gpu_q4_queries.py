@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 
 import q4ref
-from test_gpu_q4 import F32, SCORE_RTOL, Case, store, torch, vz
+from test_gpu_q4 import BF16, F32, SCORE_RTOL, Case, store, torch, vz
 from vzt import RTOL, from_dev, to_dev, widen
 
 pytestmark = pytest.mark.gpu
@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 # exact: small channels as multiples of 2^-13, which six parts below 2^13 hold exactly
 @pytest.mark.parametrize("large,exact", [(8, False), (12, False), (12, True), (16, False)])
 @pytest.mark.parametrize("length", [5, 333])
-@pytest.mark.parametrize("dtype,d,Hq,Hkv", [(F32, 128, 8, 2), (F32, 64, 8, 1), (F32, 128, 18, 2), (F32, 64, 32, 2)])
+@pytest.mark.parametrize("dtype,d,Hq,Hkv", [(F32, 128, 8, 2), (F32, 64, 8, 1), (F32, 128, 18, 2), (F32, 64, 32, 2),
+                                            (BF16, 128, 8, 2), (BF16, 64, 14, 2), (BF16, 128, 16, 1), (BF16, 64, 9, 1)])
 def test_small_channels_beside_large_ones(dtype, d, Hq, Hkv, length, large, exact):
     m, t, L, gamma = vz(), torch(), 2, 0.9
     c = Case(length + large, L, Hq, Hkv, d, length + 1, dtype)
