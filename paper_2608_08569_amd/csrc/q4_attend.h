@@ -238,7 +238,7 @@ struct Queries {
         // the first part's scale 2^e: top <= 7 2^e; its error is at most 2^(e - 2), the next one's (at 2^(e - 4))
         // 2^(e - 7), and 2^-5 of that after each further one
         int e = __builtin_amdgcn_frexp_expf(top) - (__builtin_amdgcn_frexp_mantf(top) > 0.875f ? 2 : 3);
-        e = min(max(e, -96), 125);  // (every part's scale a normal float)
+        e = min(max(e, -102), 126);  // (every part's scale a normal float)
 #pragma unroll
         for (int j = 0; j < kProducts; ++j) {
             q[j] = i32x8{0, 0, 0, 0, 0, 0, 0, 0};
