@@ -439,8 +439,8 @@ VZ_API int voxzip_unpack_q4(const void *codes, const void *scales, int64_t n_row
  * cache holds, the new slot included.  dtype is the type of q, k_new, v_new
  * and out.  Logits, softmax statistics, probabilities in the score and sums
  * are float32 in both types, logits of queries held to 2^-28 of the largest
- * channel of their block of 32 (or 2^-129); the probabilities of P V have 8 bits (bfloat16)
- * or 24 (float32).
+ * channel of their block of 32 (or 2^-129); the probabilities of P V have 16
+ * bits (bfloat16) or 24 (float32), and out is rounded to dtype once.
  *  workspace    at least voxzip_workspace_bytes(VZ_OP_DECODE_Q4, ...) bytes.
  * Errors: as voxzip_decode_attend_score.
  */

@@ -23,8 +23,10 @@
 // keys.  The accumulator layout of K Q^T (a lane: one head, keys 4 (lane / 16)
 // + i of two 16-key tiles) is the operand layout of P V with its eight
 // contraction steps taken in that key order, so p goes from one product into
-// the other in registers; in a bfloat16 call rounded to bfloat16, of which its
-// output has no more bits, in a float32 call as three bfloat16 parts (24 bits).
+// the other in registers, as bfloat16 parts: two (16 bits) in a bfloat16 call,
+// whose outputs are then off by their own rounding alone (in one part by a fifth
+// more, 2.0e-3 of their size for 1.6e-3; 48 layers of 8193 slots: 72.8 us with one,
+// 74.2 with two), three (24 bits) in a float32 call.
 #pragma once
 
 #include <math.h>

@@ -183,7 +183,7 @@ template <int DT, int D, bool RAG, bool PACK>
 __global__ __launch_bounds__(kThreads, D == 128 && !PACK ? 2 : 3) void values_kernel(const Q4Args a) {
     using R = Rows<D>;
     using E = vz::Elem<DT>;
-    constexpr int NP = DT == VZ_F32 ? 3 : 1;                     // bfloat16 parts of p
+    constexpr int NP = DT == VZ_F32 ? 3 : 2;                     // bfloat16 parts of p
     constexpr int NC = D / 16;                                   // channels per lane of V and of an output row
     constexpr int KEYS_PER_THREAD = kMostKeys / kThreads;
     __shared__ float s_sum[kWaves][kMostKeys];  // per key: the sum of p over a wave's heads

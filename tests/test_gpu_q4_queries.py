@@ -1,12 +1,13 @@
-"""Queries with channels of very different size in one block of 32, over a 4-bit
-cache whose keys are zero where the queries are large: the logits come from the
-small channels alone."""
+"""Decode steps over a 4-bit cache held to what their arithmetic allows: one
+rounding of the output, and logits of queries of any size, with channels of very
+different size in one block of 32 among them (the keys are zero where the
+queries are large, so the logits come from the small channels alone)."""
 import numpy as np
 import pytest
 
 import q4ref
 from test_gpu_q4 import BF16, F32, SCORE_RTOL, Case, store, torch, vz
-from vzt import RTOL, from_dev, to_dev, widen
+from vzt import from_dev, to_dev, widen
 
 pytestmark = pytest.mark.gpu
 
@@ -18,7 +19,8 @@ def check_step(c, q, kn, vn, length, left):
     A logit is off by that times |k| for every channel, and by float32 sums of at most six products (2^-23 of the sum
     of the terms' magnitudes each) and two more roundings of it; p = exp(s - max) / Z carries that relative to itself,
     once for its own s and once for those in Z.  An output sum over j of p_j v_j then is off by that times the sum of
-    p_j |v_j|."""
+    p_j |v_j|; in a bfloat16 call by 2^-16 of it more, p being two bfloat16 numbers there, and by its one rounding to
+    bfloat16, 2^-8 of it, and by 2^-18 of that sum for 64 float32 roundings."""
     m, t, gamma, d, dtype = vz(), torch(), 0.9, c.d, c.dtype
     cache, s, p = c.dev()
     out = t.zeros_like(to_dev(q))
@@ -38,8 +40,8 @@ def check_step(c, q, kn, vn, length, left):
     w = np.exp(z - z.max(-1, keepdims=True))
     mean = (w[..., None] * np.abs(V)).sum(2) / w.sum(-1)[..., None]
     got_o, got_s = widen(from_dev(out), dtype), from_dev(s)
-    rms = np.sqrt((ref_o ** 2).mean(-1, keepdims=True))
-    assert (np.abs(got_o - ref_o) <= RTOL[dtype] * (np.abs(ref_o) + rms) + extra * mean).all()
+    once, parts = (2.0 ** -8, 2.0 ** -16) if dtype == BF16 else (2.0 ** -24, 0)
+    assert (np.abs(got_o - ref_o) <= once * np.abs(ref_o) + (extra + parts + 2.0 ** -18) * mean).all()
     assert (np.abs(got_s - ref_s) <= (SCORE_RTOL + extra) * np.abs(ref_s)).all()
 
 
@@ -74,3 +76,10 @@ def test_queries_of_any_size(dtype, d, Hq, Hkv, power):
     q, kn, vn = (widen(x, dtype) for x in c.rows())
     q, kn, vn = store(q * 2.0 ** power, dtype), store(kn * 2.0 ** -power, dtype), store(vn, dtype)
     check_step(c, q, kn, vn, length, lambda top: np.maximum(2.0 ** -28 * top, 2.0 ** -129))
+
+
+@pytest.mark.parametrize("dtype,d,Hq,Hkv", SHAPES + [(BF16, 128, 32, 4)])
+@pytest.mark.parametrize("length", [0, 1, 5, 40, 700])
+def test_outputs_are_rounded_once(dtype, d, Hq, Hkv, length):
+    c = Case(length + 3, 2, Hq, Hkv, d, length + 1, dtype)
+    check_step(c, *c.rows(), length, lambda top: 2.0 ** -28 * top)
