@@ -396,13 +396,14 @@ VZ_API int voxzip_evict_compact_ragged(void *k_cache, void *v_cache, float *scor
  *  code c stands for 0, 1/2, 1, 3/2, 2, 3, 4, 6 (c = 0 .. 7) and their
  *  negatives (c = 8 .. 15), times 2^(b - 127), b the scale byte of the
  *  channel's block of 32.  b = 255: the block reads as NaN.  Bytes 2 .. 252
- *  and 255 are written; zero-filled memory reads as zeros.  (E2M1 elements
- *  with an E8M0 scale.)
+ *  and 255 are written; the others are read alike (zero-filled memory as
+ *  zeros, values of 2^128 and more as infinities).  (E2M1 elements with an
+ *  E8M0 scale.)
  *  Quantising a row: per block e is the smallest of -125 .. 125 with
  *  max |x| <= 7 * 2^e (125 if there is none), b = e + 127, and each channel
  *  gets the code nearest x / 2^e, ties to the even code, at most 6 in
  *  magnitude.  A block with an infinity or a NaN gets b = 255.
- *  Every value is exact in bfloat16 and float32.
+ *  Every value written is exact in bfloat16 and float32.
  *  Codes must lie on 16-byte boundaries, scales on d / 32-byte ones
  *  (VZ_ERR_INVALID); planes have at most 2^26 slots (VZ_ERR_SHAPE).
  */
