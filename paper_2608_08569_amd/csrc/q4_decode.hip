@@ -19,11 +19,13 @@
 // a key is the sum of its final probabilities in float32, with nothing kept per
 // (key, head): forming the logits a second time reads 68 bytes of K again per
 // key and KV head (d = 128), mostly from the memory-side cache, where keeping
-// eight heads' float32 logits would write and read 64.
+// eight heads' float32 logits would write and read 64 (counted, not measured).
 //
 // Bound by reading K twice and V once.  48 layers, 32 heads on 4, d = 128, 8193
-// slots: statistics 25 us (4.2 TB/s), values 43 us (5.0 TB/s), finish 5 us; one
-// layer of 1025 slots: 4.5, 6.8 and 3.9 us, three launches' latency.
+// slots: statistics 25.9 us (4.1 TB/s), values 46.2 us (4.7 TB/s), finish 5 us;
+// one layer of 1025 slots: 4.8, 6.9 and 2.9 us, three launches' latency, which
+// makes such a step slower than over a bfloat16 cache (13.6 us from a graph for
+// 10.0).
 #include "q4_attend.h"
 
 namespace {
@@ -450,6 +452,10 @@ bool packs(int32_t Hq, int32_t Hkv) { return Hq / Hkv <= 8; }
 // - no fewer than kMostKeys asks for;
 // - where that gives every CU one, as many as give each the same number (13,181
 //   keys of 48 layers: 109 us in 13 chunks a layer, 103 in 16).
+// The host knows of a ragged call's keys only the slots that the planes have, so
+// partly filled slots get longer chunks than their keys ask for (one layer of 16
+// sequences of 2000 keys, 4 KV heads: 21 us in slots of 2017, 22 of 8068, 43 of
+// 32,272).
 constexpr int kCus = 256;
 int64_t chunks_for(int32_t L, int32_t Hkv, int64_t keys, int32_t n_seqs) {
     const int64_t rounds = keys * L / (kUnit * shares_of(Hkv));
