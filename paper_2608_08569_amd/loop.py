@@ -115,9 +115,14 @@ class DecodeLoop:
         self.length.copy_(self.torch.from_numpy(lengths))
         self.next_pos.copy_(self.torch.from_numpy(lengths if next_pos is None else np.asarray(next_pos, np.int32)))
 
+    def _check_prefill(self, k_in):
+        if k_in.dtype != self.out.dtype:  # (a 4-bit cache's planes would take either type)
+            raise TypeError(f"prefill has dtype {k_in.dtype}, expected {self.out.dtype}")
+
     def fuse(self, k_in, v_in, in_base, T_in, span_off, off_base, n_spans, max_spans):
         """Stage-1 fusion of every sequence's prefill into the packed cache;
         lengths and positions start at the span counts."""
+        self._check_prefill(k_in)
         self._fuse_call(k_in, v_in, in_base, T_in, span_off, off_base, n_spans, max_spans, *self.planes, self.score,
                         self.pos, self.seq_base, self.cap, status=self.status)
         self.length.copy_(n_spans)
@@ -147,6 +152,7 @@ class DecodeLoop:
         L, H, T_in, d = k_in.shape
         if (L, H, d) != (self.L, self.Hkv, self.d):
             raise ValueError(f"prefill has shape {tuple(k_in.shape)}, expected [{self.L}][{self.Hkv}][T][{self.d}]")
+        self._check_prefill(k_in)
         n_spans = int(span_off.numel()) - 1
         if n_spans < 1 or n_spans + 1 > self.slot_cap[s]:
             raise ValueError(f"{n_spans} spans do not fit slot {s} of {self.slot_cap[s]} slots with a free one")
